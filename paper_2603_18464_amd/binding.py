@@ -24,7 +24,8 @@ EXPORTS = ["vla_create", "vla_destroy", "vla_last_error", "vla_query_sizes", "vl
            "vla_batcher_create", "vla_batcher_destroy", "vla_batcher_push", "vla_batcher_size",
            "vla_batcher_deadline", "vla_batcher_poll",
            "vla_get_state", "vla_drain_begin", "vla_update_begin", "vla_update_tensors", "vla_update_commit",
-           "vla_prof_enable", "vla_prof_count", "vla_prof_read"]
+           "vla_prof_enable", "vla_prof_count", "vla_prof_read",
+           "vla_loss_workspace", "vla_token_loss", "vla_token_loss_grad", "vla_distill_loss", "vla_distill_loss_grad"]
 
 
 class vla_config(C.Structure):
@@ -43,6 +44,12 @@ class vla_tensor(C.Structure):
 
 class vla_request(C.Structure):
     _fields_ = [("id", C.c_uint64), ("n_patches", C.c_int32), ("n_instr", C.c_int32), ("t_arrival", C.c_double)]
+
+
+class vla_head_rows(C.Structure):
+    _fields_ = [("hidden", C.c_void_p), ("head", C.c_void_p), ("ld_hidden", C.c_int64), ("ld_head", C.c_int64),
+                ("n_rows", C.c_int32), ("d_model", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("temperature", C.c_float)]
 
 
 class VlaError(RuntimeError):
@@ -105,6 +112,12 @@ def lib() -> C.CDLL:
         L.vla_batcher_deadline.argtypes = [vp, C.POINTER(C.c_double)]
         L.vla_batcher_poll.argtypes = [vp, C.c_double, C.POINTER(vla_request), i32, C.POINTER(C.c_int32)]
         L.vla_select.argtypes = [vp, i32, vp, f32, vp, i32, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp]
+        rows, size = C.POINTER(vla_head_rows), C.c_size_t
+        L.vla_loss_workspace.argtypes = [rows, i32, i32, C.POINTER(size)]
+        L.vla_token_loss.argtypes = [rows, vp, vp, vp, vp, size, vp]
+        L.vla_token_loss_grad.argtypes = [rows, vp, vp, vp, vp, vp, vp, size, vp]
+        L.vla_distill_loss.argtypes = [rows, vp, vp, i32, vp, vp, vp, size, vp]
+        L.vla_distill_loss_grad.argtypes = [rows, vp, vp, i32, vp, vp, vp, vp, vp, size, vp]
         L.vla_prof_enable.argtypes = [vp, i32]
         L.vla_prof_count.argtypes = []
         L.vla_prof_read.argtypes = [vp, i32, C.POINTER(C.c_char_p), C.POINTER(C.c_int64), C.POINTER(C.c_double)]
@@ -301,6 +314,40 @@ def vla_gemm_first_rows(rows: int, n: int, k: int, two_term: bool, span: int) ->
 
 def vla_decode_reads_once(ctx, rows: int, positions: int) -> int:
     return lib().vla_decode_reads_once(ctx, rows, positions)
+
+
+def _check_loss(rc: int, name: str):
+    if rc != 0:
+        raise VlaError(rc, name)
+
+
+def vla_loss_workspace(rows: vla_head_rows, n_top: int = 0, grad: bool = False) -> int:
+    n = C.c_size_t()
+    _check_loss(lib().vla_loss_workspace(C.byref(rows), n_top, int(grad), C.byref(n)), "vla_loss_workspace")
+    return n.value
+
+
+def vla_token_loss(rows: vla_head_rows, labels, loss_out, lse_out, work, stream: int = 0) -> None:
+    _check_loss(lib().vla_token_loss(C.byref(rows), _ptr(labels), _ptr(loss_out), _ptr(lse_out), _ptr(work),
+                                     work.numel() if work is not None else 0, stream), "vla_token_loss")
+
+
+def vla_token_loss_grad(rows: vla_head_rows, labels, lse, grad_loss, grad_hidden, grad_head, work, stream: int = 0) -> None:
+    _check_loss(lib().vla_token_loss_grad(C.byref(rows), _ptr(labels), _ptr(lse), _ptr(grad_loss), _ptr(grad_hidden),
+                                          _ptr(grad_head), _ptr(work), work.numel() if work is not None else 0, stream),
+                "vla_token_loss_grad")
+
+
+def vla_distill_loss(rows: vla_head_rows, top_logits, top_ids, n_top: int, loss_out, lse_out, work, stream: int = 0) -> None:
+    _check_loss(lib().vla_distill_loss(C.byref(rows), _ptr(top_logits), _ptr(top_ids), n_top, _ptr(loss_out), _ptr(lse_out),
+                                       _ptr(work), work.numel() if work is not None else 0, stream), "vla_distill_loss")
+
+
+def vla_distill_loss_grad(rows: vla_head_rows, top_logits, top_ids, n_top: int, lse, grad_loss, grad_hidden, grad_head, work,
+                          stream: int = 0) -> None:
+    _check_loss(lib().vla_distill_loss_grad(C.byref(rows), _ptr(top_logits), _ptr(top_ids), n_top, _ptr(lse), _ptr(grad_loss),
+                                            _ptr(grad_hidden), _ptr(grad_head), _ptr(work),
+                                            work.numel() if work is not None else 0, stream), "vla_distill_loss_grad")
 
 
 def vla_prof_enable(ctx, mask: int) -> None:

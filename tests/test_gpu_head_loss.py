@@ -1,0 +1,229 @@
+"""The head's losses against the oracle in 64 bits, elementwise, within bounds counted in roundings (oracle/loss_oracle.py)."""
+import math
+
+import pytest
+import torch
+
+import paper_2603_18464_amd as P
+from oracle.loss_oracle import Loss, target
+from paper_2603_18464_amd.losses import loss_workspace
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def inputs(T, d, V, dtype, seed=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed + 1000 * T + V)
+    W = (0.05 * torch.randn(V, d, generator=g)).to(TYPES[dtype])
+    y = torch.randint(0, V, (T,), generator=g, dtype=torch.int32)
+    h = torch.randn(T, d, generator=g) + 4.0 / (0.05 * math.sqrt(d)) * W[y.long()].float() / 0.05 / math.sqrt(d) * torch.rand(T, 1, generator=g)
+    coef = torch.randn(T, generator=g) / T
+    return (h * scale).to(TYPES[dtype]).to(DEV), W.to(DEV), y.to(DEV), coef.to(DEV), g
+
+
+def teacher(T, V, k, g):
+    ids = torch.randint(-1, V + 1, (T, k), generator=g, dtype=torch.int32)            # some missing, some twice
+    logits = 3.0 * torch.randn(T, k, generator=g)
+    logits[torch.rand(T, k, generator=g) < 0.1] = -math.inf
+    logits[(ids < 0) | (ids >= V)] = math.nan                                         # what is not there may hold anything
+    return logits.to(DEV), ids.to(DEV)
+
+
+def call(kind, h, W, tgt, tau, coef, work_fill=0xFF):
+    """loss, lse, grads of the calls, in workspaces that hold garbage and are followed by bytes nobody may touch."""
+    k = tgt[1].shape[1] if kind == "distill" else 0
+
+    def work(grad):
+        n = loss_workspace(h, W, k, grad)
+        w = torch.full((n + 4096,), work_fill, dtype=torch.uint8, device=DEV)
+        return w, n
+    loss_f, grad_f = (P.token_loss, P.token_loss_grad) if kind == "token" else (P.distill_loss, P.distill_loss_grad)
+    w1, n1 = work(False)
+    w2, n2 = work(True)
+    loss, lse = loss_f(h, W, *tgt, temperature=tau, work=w1[:n1])
+    gh, gw = grad_f(h, W, *tgt, lse, coef, temperature=tau, work=w2[:n2])
+    torch.cuda.synchronize()
+    assert bool((w1[n1:] == work_fill).all()) and bool((w2[n2:] == work_fill).all())
+    return loss, lse, gh, gw
+
+
+def within(got, want, bound, what):
+    err = (got.double() - want).abs()
+    bad = ~(err <= bound)
+    assert not bool(bad.any()), (what, int(bad.sum()), float(err[bad].max()), float((err / bound.clamp_min(1e-300))[bad].max()))
+
+
+def check(kind, h, W, tgt, tau, coef, got):
+    r = target(W.shape[0], **(dict(labels=tgt[0]) if kind == "token" else dict(top_logits=tgt[0], top_ids=tgt[1])), tau=tau or 1.0)
+    o = Loss(h, W, r, tau or 1.0)
+    loss, lse, b_loss, b_lse = o.loss_bounds()
+    within(got[0], loss, b_loss, "loss")
+    within(got[1], lse, b_lse, "lse")
+    (gh, bh), (gw, bw) = o.grad_bounds(coef)
+    within(got[2], gh, bh, "grad_hidden")
+    within(got[3], gw, bw, "grad_head")
+
+
+SIZES = [(1, 8, 1), (1, 64, 2), (1, 128, 200), (3, 264, 65), (28, 256, 256), (33, 136, 129), (63, 64, 63), (64, 128, 257), (65, 768, 1000),
+         (100, 72, 2000), (129, 512, 700), (200, 1536, 333), (257, 128, 5000), (700, 256, 2500), (1025, 64, 300)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,V", SIZES)
+def test_token(T, d, V, dtype):
+    h, W, y, coef, _ = inputs(T, d, V, dtype)
+    y[::5] = torch.tensor([-1, V, -100, 2 ** 31 - 1], dtype=torch.int32, device=DEV).repeat(T // 20 + 1)[:len(y[::5])]
+    if T == 1:
+        y[0] = V - 1
+    idle = (y < 0) | (y >= V)
+    h[idle] = math.nan
+    h[idle.nonzero()[:1, 0]] = math.inf
+    coef[idle] = math.nan
+    tau = (0.0, 1.0, 0.6)[T % 3]
+    check("token", h, W, (y,), tau, torch.where(idle, 0.0, coef), call("token", h, W, (y,), tau, coef))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d,V", SIZES)
+@pytest.mark.parametrize("k", [1, 7, 100])
+def test_distill(T, d, V, k, dtype):
+    h, W, _, coef, g = inputs(T, d, V, dtype, seed=k)
+    logits, ids = teacher(T, V, k, g)
+    if T == 1:
+        ids[0, 0], logits[0, 0] = 0, 1.0
+    idle = ~((ids >= 0) & (ids < V) & (logits != -math.inf)).any(1)
+    h[idle] = math.nan
+    tau = (0.0, 1.7, 0.6)[T % 3]
+    tgt = (logits, ids)
+    check("distill", h, W, tgt, tau, coef, call("distill", h, W, tgt, tau, coef))
+
+
+def test_lists_of_the_largest_length_in_one_corner_of_the_vocabulary():
+    T, d, V, k = 5, 128, 1500, 1024
+    h, W, _, coef, g = inputs(T, d, V, "bf16")
+    ids = torch.stack([torch.randperm(V, generator=g)[:k] if t % 2 else torch.randint(0, 40, (k,), generator=g) for t in range(T)]).to(torch.int32).to(DEV)
+    logits = torch.randn(T, k, generator=g).to(DEV)
+    check("distill", h, W, (logits, ids), 1.0, coef, call("distill", h, W, (logits, ids), 1.0, coef))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pieces_of_the_vocabulary(dtype):
+    """Sizes whose gradient takes several pieces, the last one not full."""
+    T, d, V = (1500, 64, 20001) if dtype == "f32" else (4100, 64, 20001)
+    h, W, y, coef, _ = inputs(T, d, V, dtype)
+    check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_further_apart_and_other_streams(dtype):
+    T, d, V = 70, 192, 500
+    h0, W0, y, coef, _ = inputs(T, d, V, dtype)
+    wide_h = torch.full((T, d + 40), math.nan, dtype=h0.dtype, device=DEV)
+    wide_W = torch.full((V, d + 8), math.nan, dtype=h0.dtype, device=DEV)
+    wide_h[:, 16:16 + d], wide_W[:, 8:8 + d] = h0, W0
+    h, W = wide_h[:, 16:16 + d], wide_W[:, 8:8 + d]
+    dense = call("token", h0, W0, (y,), 0.0, coef)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        loss, lse = P.token_loss(h, W, y)
+        gh, gw = P.token_loss_grad(h, W, y, lse, coef)
+    s.synchronize()
+    for a, b in zip((loss, lse, gh, gw), dense):
+        assert torch.equal(a, b)
+    with pytest.raises(P.VlaError):
+        P.token_loss(wide_h[:, 1:1 + d], W, y)                          # not on 16 bytes
+    with pytest.raises(P.VlaError):
+        P.token_loss(h0.T.contiguous().T, W0, y)                        # columns apart
+    with pytest.raises(P.VlaError):
+        P.token_loss(h0[:1].expand(T, d), W0, y)                        # one row for all
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scales(dtype):
+    """Rows from 1e-20 to 1e6 beside one another, coefficients from 1e-12 to 1e6, a row of zeros, a coefficient of zero."""
+    T, d, V = 96, 128, 300
+    h, W, y, coef, _ = inputs(T, d, V, dtype)
+    s = torch.logspace(-20, 0, T, device=DEV)
+    h = (h.float() * s[:, None]).to(h.dtype)
+    h[17] = 0
+    h[20] *= 1e6 / float(h[20].float().abs().max())
+    W = (W.float() / 1e3).to(W.dtype)
+    coef = torch.logspace(6, -12, T, device=DEV) * coef.sign()
+    coef[30] = 0
+    check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
+
+
+def test_no_row_has_a_target():
+    h, W, y, coef, _ = inputs(40, 128, 300, "bf16")
+    h[:] = math.nan
+    for out in call("token", h, W, (torch.full_like(y, -100),), 0.0, coef):
+        assert bool((out == 0).all())
+    ids = torch.full((40, 3), -1, dtype=torch.int32, device=DEV)
+    for out in call("distill", h, W, (torch.full((40, 3), math.nan, device=DEV), ids), 0.0, coef):
+        assert bool((out == 0).all())
+
+
+def test_values_that_are_not_finite_reach_their_row_and_nothing_is_made_up():
+    h, W, y, coef, _ = inputs(40, 128, 300, "bf16")
+    h[3, 5], h[7, 0] = math.nan, math.inf
+    loss, lse, gh, gw = call("token", h, W, (y,), 0.0, coef)
+    bad = torch.zeros(40, dtype=torch.bool, device=DEV)
+    bad[3] = bad[7] = True
+    assert torch.equal(~torch.isfinite(loss), bad) and torch.equal(~torch.isfinite(gh).all(1), bad)
+    assert not bool(torch.isfinite(gw).any())
+    W[9, 4] = 1000.0                                                     # beyond what the half-precision form of W holds
+    loss, *_ = call("token", h, W, (y,), 0.0, coef)
+    assert not bool(torch.isfinite(loss).any())
+
+
+def test_one_gradient_alone_and_the_same_bits_again():
+    h, W, y, coef, _ = inputs(150, 256, 1000, "bf16")
+    loss, lse, gh, gw = call("token", h, W, (y,), 0.0, coef)
+    assert torch.equal(P.token_loss_grad(h, W, y, lse, coef, want_head=False)[0], gh)
+    assert torch.equal(P.token_loss_grad(h, W, y, lse, coef, want_hidden=False)[1], gw)
+    for _ in range(3):
+        for a, b in zip(call("token", h, W, (y,), 0.0, coef, work_fill=0x3C), (loss, lse, gh, gw)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_rows_loss_does_not_depend_on_the_rows_beside_it(dtype):
+    h, W, y, _, _ = inputs(600, 256, 1000, dtype)
+    loss, lse = P.token_loss(h, W, y)
+    for a, n in ((0, 1), (5, 33), (599, 1), (100, 300)):
+        l2, s2 = P.token_loss(h[a:a + n], W, y[a:a + n])
+        assert torch.equal(l2, loss[a:a + n]) and torch.equal(s2, lse[a:a + n])
+
+
+@pytest.mark.parametrize("kind", ["token", "distill"])
+def test_captured_and_replayed(kind):
+    """A graph of both calls, replayed with other contents, with eager work and waits between the replays."""
+    T, d, V, k = 90, 256, 700, 9
+    h, W, y, coef, g = inputs(T, d, V, "bf16")
+    tgt = (y,) if kind == "token" else teacher(T, V, k, g)
+    loss_f, grad_f = (P.token_loss, P.token_loss_grad) if kind == "token" else (P.distill_loss, P.distill_loss_grad)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        _, lse0 = loss_f(h, W, *tgt)
+        grad_f(h, W, *tgt, lse0, coef)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, lse = loss_f(h, W, *tgt)
+        gh, gw = grad_f(h, W, *tgt, lse, coef)
+    for seed in range(4):
+        h2, _, y2, coef2, g2 = inputs(T, d, V, "bf16", seed=50 + seed)
+        h.copy_(h2)
+        coef.copy_(coef2)
+        for a, b in zip(tgt, (y2,) if kind == "token" else teacher(T, V, k, g2)):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        want_loss, want_lse = loss_f(h, W, *tgt)
+        want_gh, want_gw = grad_f(h, W, *tgt, want_lse, coef)
+        torch.cuda.synchronize()
+        for a, b in ((loss, want_loss), (lse, want_lse), (gh, want_gh), (gw, want_gw)):
+            assert torch.equal(a, b)
