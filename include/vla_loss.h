@@ -37,7 +37,7 @@ extern "C" {
 #endif
 
 /* Rows and head of a call.  Rows may be further apart than d_model (ld_*, in elements); both start on 16 bytes and ld is a
- * multiple of 16 bytes.  1 <= n_rows, vocab <= 2^20; d_model <= 2^15, a multiple of 8 (VLA_BF16) or 4 (VLA_F32). */
+ * multiple of 16 bytes, at most 2^22 elements.  1 <= n_rows, vocab <= 2^20; d_model <= 2^15, a multiple of 8 (VLA_BF16) or 4 (VLA_F32). */
 typedef struct {
   const void* hidden;        /* device, [n_rows, d_model] */
   const void* head;          /* device, [vocab, d_model] */
@@ -59,7 +59,8 @@ int vla_token_loss(const vla_head_rows* rows, const int32_t* labels, float* loss
 int vla_distill_loss(const vla_head_rows* rows, const float* top_logits, const int32_t* top_ids, int32_t n_top,
                      float* loss_out, float* lse_out, void* work, size_t work_bytes, void* hip_stream);
 
-/* lse: as the loss call returned it; grad_loss: device, [n_rows] float32.  grad_hidden [n_rows, d_model] and grad_head
+/* lse: as the loss call returned it (VLA_F32 forms its own: a gradient with float32's precision takes the normaliser of the very
+ * logits it forms); grad_loss: device, [n_rows] float32.  grad_hidden [n_rows, d_model] and grad_head
  * [vocab, d_model], without gaps, in the storage dtype, are overwritten; one of the two may be NULL (not wanted). */
 int vla_token_loss_grad(const vla_head_rows* rows, const int32_t* labels, const float* lse, const float* grad_loss,
                         void* grad_hidden, void* grad_head, void* work, size_t work_bytes, void* hip_stream);

@@ -174,6 +174,49 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[MT][NT]) {
 
 constexpr int PK = 64;                                 // k of a slab (a slab of low terms is one 128-deep product)
 
+// What an epilogue may ask of the kernel besides:
+//   kRaw 1: W is not packed but bfloat16 rows [N, K], raw_ld apart, of which raw_rows exist: re-encoded (w * kWeightScale)
+//        between the LDS and the matrix cores.  K % 64 == 0.
+//   kRaw 2: W is bfloat16 rows [K, N], raw_ld apart, of which raw_rows (contraction) and raw_cols (a multiple of 8) exist;
+//        read transposed from the LDS.  raw_rows > K - 64; A must be zero where its contraction goes past raw_rows.
+//   kSliced: tiles of each of `slices` slices of the contraction; slice() is told which one.
+//   begin(lane): once a wave, in front of the first consume.
+template <class Epi> consteval int raw_w() {
+  if constexpr (requires { Epi::kRaw; }) return Epi::kRaw;
+  else return 0;
+}
+template <class Epi> consteval bool sliced() {
+  if constexpr (requires { Epi::kSliced; }) return Epi::kSliced;
+  else return false;
+}
+template <class Epi> __device__ __forceinline__ int raw_rows_of(const Epi& e) {
+  if constexpr (requires { e.raw_rows; }) return e.raw_rows;
+  else return 1;
+}
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+// Four k of one column a lane, of a block of 4 k x 16 columns that 16 lanes address in pieces of four columns (no wait).
+template <int OFF>
+__device__ __forceinline__ void read_transposed_asm(u32x2& dst, unsigned addr) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF) : "memory");
+#endif
+}
+__device__ __forceinline__ void hold(u32x2& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
+}
+// Eight bfloat16 weights as the half-precision operands of the matrix cores.
+__device__ __forceinline__ f16x8 encode_weights(const u32x4& v) {
+  f16x8 o;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    o[2 * j] = (f16)(__builtin_bit_cast(float, v[j] << 16) * kWeightScale);
+    o[2 * j + 1] = (f16)(__builtin_bit_cast(float, v[j] & 0xffff0000u) * kWeightScale);
+  }
+  return o;
+}
+
 template <class Epi> __device__ __forceinline__ const f16* epi_a_lo(const Epi&) { return nullptr; }
 
 // The accumulators of a wave's 16 MT x 16 NT, rows m_wave .. and column group wn of a tile's columns n0 .., through LDS to the
@@ -253,9 +296,15 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
   // at 18560 rows, where the L2 then holds too few weight columns).
   const int nblk = tiles_m * tiles_n;
   const int per_xcd = gridDim.x >> 3;
-  const int pid = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (pid >= nblk) return;
+  int pid = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   int tm, tn, kz = 0;
+  if constexpr (sliced<Epi>()) {
+    kz = pid / nblk;
+    if (kz >= epi_in.slices) return;
+    pid -= kz * nblk;
+  } else if (pid >= nblk) {
+    return;
+  }
   if constexpr (SPLITK) {                              // consecutive workgroups of an XCD share a K slice (the A slabs)
     tm = 0;
     tn = pid % tiles_n;
@@ -286,6 +335,12 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
     KT = K > Kw ? 2 * KTw : KTw;                       // the low-term slabs of the slice follow its high-term slabs
     epi.part += (size_t)kz * epi.plane_rows * epi.N;
   }
+  if constexpr (sliced<Epi>()) {
+    const int u0 = (int)((long long)kz * KTw / epi.slices), u1 = (int)((long long)(kz + 1) * KTw / epi.slices);
+    kb0 = (size_t)u0 * KS16;
+    KT = KTw = u1 - u0;
+    epi.slice(kz);
+  }
 
   const unsigned lane16 = (unsigned)lane * 16u;        // lane offset in an operand in fragment order
   const f16* a_base = A + (size_t)m0 * lda + kb0 * 512;
@@ -298,6 +353,29 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
   // runs ahead of the others of the same columns and XCD, which find the weights in the L2.  us with whole blocks / this, cold
   // weights, N 4096: 580 rows K 4096 41.2 / 38.7, K 11008 94 / 88, with low terms 137 / 127; 1160 rows 61 / 57.6, 138 / 133.
   const unsigned lane_last = (unsigned)(min(lane & 31, (M - 1 - m0) & 31) + (lane & 32)) * 16u;      // in block a_last
+  // Unpacked W: a wave's pieces of a KiB are 8 rows of 64 k, or 1024 / (2 BN) rows of the contraction, 16 bytes a lane.  The chunks
+  // of 16 bytes of a row are swizzled so that the reads of the LDS have no more bank conflicts than bytes: by the row
+  // (reads of 16 rows), and in pairs (32 bytes) by the rows of the contraction that a transposed read takes together.
+  constexpr int RAW = raw_w<Epi>();
+  static_assert(!RAW || (!LO8 && !AGPR && !SPLITK), "products left to the compiler, one pass");
+  [[maybe_unused]] unsigned raw_off[RAW ? WP : 1], raw_row[RAW == 2 ? WP : 1];
+  [[maybe_unused]] const int raw_n0 = RAW == 1 ? min(n0, raw_rows_of(epi_in) - 1) : 0;      // (a tile may be all padding)
+  if constexpr (RAW == 1) {
+#pragma unroll
+    for (int i = 0; i < WP; ++i) {
+      const int row = (wave * WP + i) * 8 + (lane >> 3);
+      raw_off[i] = (unsigned)min(row, epi.raw_rows - 1 - raw_n0) * 2u * (unsigned)epi.raw_ld + (unsigned)((lane & 7) ^ ((row >> 1) & 7)) * 16u;
+    }
+  }
+  constexpr int RPP = RAW == 2 ? 512 / BN : 1;         // rows of a piece
+  if constexpr (RAW == 2) {
+#pragma unroll
+    for (int i = 0; i < WP; ++i) {
+      const int row = (wave * WP + i) * RPP + lane / (64 / RPP), f = (row & 3) | ((row >> 3) & 1) << 2;
+      raw_row[i] = row;
+      raw_off[i] = (unsigned)min(n0 / 8 + ((lane % (64 / RPP)) ^ (f << 1)), epi.raw_cols / 8 - 1) * 16u;
+    }
+  }
   const int a_back = REST ? wave - wave % (REST ? REST : 1) : 0;     // pieces a wave's last one is moved back by
   auto issue_one = [&](int kt, auto I) VLA_INLINE {    // piece I of this wave's share of slab kt (clamped), A first
     constexpr int i = decltype(I)::value;
@@ -309,6 +387,16 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
       load_to_lds_16(low ? a_lo_base : a_base, j / KS16 < a_last ? lane16 : j / KS16 == a_last ? lane_last : 0u, blk + 1024u * KS16 * (unsigned)(SPLITK ? kw : ks), lds + (kt % S) * A_STAGE + j * 512);
     } else {
       const int j = wave * WP + i - AP;                // piece of the slab: block row j / KS16, 16-k block j % KS16
+      if constexpr (RAW == 1) {
+        load_to_lds_16((const f16*)Wp + (size_t)raw_n0 * epi.raw_ld + kb0 * 16, raw_off[i - AP], 128u * (unsigned)kw, lds + W0_HALVES + (kt % SW) * W_STAGE + j * 512);
+        return;
+      }
+      if constexpr (RAW == 2) {
+        const size_t k0 = kb0 * 16 + (size_t)kw * PK;
+        const unsigned row = min(raw_row[i - AP], (unsigned)(epi.raw_rows - 1 - (int)k0));
+        load_to_lds_16((const f16*)Wp + k0 * epi.raw_ld, raw_off[i - AP] + row * 2u * (unsigned)epi.raw_ld, 0u, lds + W0_HALVES + (kt % SW) * W_STAGE + j * 512);
+        return;
+      }
       const bool low = LO8 && ks >= KTw;
       const unsigned blk = (unsigned)(j / KS16 * KB16) * (low ? 512u : 1024u) + (unsigned)(j % KS16) * 1024u;
       load_to_lds_16(low ? w8_base : w_base, lane16, blk + 1024u * KS16 * (unsigned)kw, lds + W0_HALVES + (kt % SW) * W_STAGE + j * 512);
@@ -339,6 +427,20 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
 
   constexpr int NBUF = DEEP ? 2 * KS : 2;              // register buffers, a k-step each
   f16x8 af[NBUF][MT], bf[NBUF][NT];
+  [[maybe_unused]] u32x2 bt[RAW == 2 ? NBUF : 1][NT][2];     // transposed reads
+  [[maybe_unused]] f16x8 bc[RAW ? NT : 1];                   // of the k-step, re-encoded
+  [[maybe_unused]] unsigned w_raw[RAW == 2 ? NT : 2];
+  if constexpr (RAW == 1) {
+#pragma unroll
+    for (int ss = 0; ss < 2; ++ss)
+      w_raw[ss] = lds0 + 2u * (unsigned)W0_HALVES + (unsigned)(wn * WN + (lane & 15)) * 128u + (unsigned)((4 * ss + fgrp) ^ ((lane & 15) >> 1)) * 16u;
+  }
+  if constexpr (RAW == 2) {
+    const unsigned row = (unsigned)(8 * fgrp + ((lane & 15) >> 2)), f = ((lane >> 2) & 3) | (fgrp & 1) << 2;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      w_raw[nt] = lds0 + 2u * (unsigned)W0_HALVES + row * (2u * BN) + ((unsigned)(wn * NT + nt) ^ f) * 32u + (unsigned)(lane & 3) * 8u;
+  }
   constexpr int R = MT + NT, MF = MT * NT;             // reads and products of a k-step
   struct Stages { unsigned a, b; };                    // byte offsets of a slab's stages
   auto stages_of = [&](int kt) VLA_INLINE {
@@ -352,19 +454,31 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
   };
   auto read_b = [&](Stages so, f16x8& dst, auto SS, auto J) VLA_INLINE {
     constexpr int ss = decltype(SS)::value, j = decltype(J)::value;
-    read_frag_asm<(j / 2 * KS16 + 2 * ss) * 1024 + (j & 1) * 256>(dst, w_b + so.b);
+    if constexpr (RAW == 1) read_frag_asm<j * 2048>(dst, w_raw[ss] + so.b);
+    else read_frag_asm<(j / 2 * KS16 + 2 * ss) * 1024 + (j & 1) * 256>(dst, w_b + so.b);
   };
   auto read_one = [&](Stages so, int f, auto SS, auto I) VLA_INLINE {   // I-th fragment read of a k-step
     constexpr int x = decltype(I)::value;
     if constexpr (x < MT) read_a(so, af[f][x], SS, I);
-    else read_b(so, bf[f][x - MT], SS, std::integral_constant<int, x - MT>{});
+    else if constexpr (RAW == 2) {
+      constexpr int off = 32 * decltype(SS)::value * 2 * BN;
+      read_transposed_asm<off>(bt[f][x - MT][0], w_raw[x - MT] + so.b);
+      read_transposed_asm<off + 4 * 2 * BN>(bt[f][x - MT][1], w_raw[x - MT] + so.b);
+    } else read_b(so, bf[f][x - MT], SS, std::integral_constant<int, x - MT>{});
   };
   auto arrived = [&](int f) VLA_INLINE {
     wait_lds();
 #pragma unroll
     for (int i = 0; i < MT; ++i) hold(af[f][i]);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) hold(bf[f][j]);
+    for (int j = 0; j < NT; ++j) {
+      if constexpr (RAW == 2) {
+        hold(bt[f][j][0]);
+        hold(bt[f][j][1]);
+      } else {
+        hold(bf[f][j]);
+      }
+    }
   };
   // One k-step of slab kt: the MFMAs, and between them fragment reads (in the first three quarters, so that they have
   // landed at the end) and the loads that take slab kt's stages (A of slab kt + S, W of slab kt + SW).
@@ -383,7 +497,12 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
     const Stages so = stages_of(kt + (next ? 1 : 0));
     static_for<MF>([&](auto I) VLA_INLINE {
       constexpr int i = decltype(I)::value, mt = i / NT, nt = i % NT;
-      if constexpr (LO8 || AGPR) mfma_in_place<AGPR>(acc[mt][nt], af[f][mt], bf[f][nt]);
+      if constexpr (RAW && mt == 0) {
+        if constexpr (RAW == 2) bc[nt] = encode_weights(u32x4{bt[f][nt][0][0], bt[f][nt][0][1], bt[f][nt][1][0], bt[f][nt][1][1]});
+        else bc[nt] = encode_weights(__builtin_bit_cast(u32x4, bf[f][nt]));
+      }
+      if constexpr (RAW != 0) acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(af[f][mt], bc[nt], acc[mt][nt], 0, 0, 0);
+      else if constexpr (LO8 || AGPR) mfma_in_place<AGPR>(acc[mt][nt], af[f][mt], bf[f][nt]);
       else acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(af[f][mt], bf[f][nt], acc[mt][nt], 0, 0, 0);
       constexpr int r0 = i < n_rd ? i * R / n_rd : R, r1 = i < n_rd ? (i + 1) * R / n_rd : R;
       static_for<r1 - r0>([&](auto J) VLA_INLINE {
@@ -515,13 +634,16 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
   wait_vmcnt<0>();                                     // the clamped tail loads still target this workgroup's LDS
   __syncthreads();                                     // every wave is done with the slabs: LDS becomes epilogue staging
 
+  if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
   store_tile<MT, NT, WGN>(acc, epi, smem, wave, wn, lane, m0 + wm * WM, n0, M);
 }
 
 template <int WGM, int WGN, int WM, int WN, int S, int SW, int OCC, bool DEEP, bool SPREAD, bool LO8, bool SPLITK, class Epi>
 static void launch_tiles(const f16* A, int lda, const f16* Wp, const f16* W8, int M, int K, int Kw, int tiles_m,
                          int tiles_n, const Epi& epi, hipStream_t st) {
-  const int grid = (tiles_m * tiles_n + 7) / 8 * 8;
+  int wgs = tiles_m * tiles_n;
+  if constexpr (sliced<Epi>()) wgs *= epi.slices;
+  const int grid = (wgs + 7) / 8 * 8;
   constexpr size_t slabs = ((size_t)S * WGM * WM + (size_t)SW * WGN * WN) * PK * sizeof(f16);
   constexpr bool pair = WN < Epi::kSpan;
   constexpr size_t stage = (size_t)WGM * WGN / (pair ? 2 : 1) * 32 * ((pair ? 2 : 1) * WN + 4) * sizeof(float);

@@ -7,10 +7,10 @@
 // The gradient forms z again, dz = q - r with q = exp(z - lse), and two products: grad_hidden = (g / tau) dz W, where a row's
 // coefficient is applied at the end, and grad_head = dz^T (g h / tau), where it is applied to h.
 //
-// All products run on the half-precision kernel of gemm_tile.h, whose operands are in fragment order.  Powers of two keep them in
-// the range of half precision: a row of h is scaled to a maximum in [2^13, 2^14) (exact for bfloat16), W by 2^8 (exact, as
-// in the arena), dz, which lies in [-1, 1], by 2^15, and g h / tau as one tensor to a maximum in [2^13, 2^14).  dz is rounded to
-// half precision (2^-11 of its value at most) and g h / tau likewise; everything else is float32.
+// All products run on the half-precision kernel of gemm_tile.h.  Powers of two keep operands in the range of half precision: a
+// row of h is scaled to a maximum in [2^13, 2^14) (exact for bfloat16), W by 2^8 (exact, as in the arena), dz, which lies in
+// [-1, 1], by 2^15 for grad_hidden, whose rows take their g / tau at the end, and times g / tau over the row's scale as one tensor
+// to a maximum of 2^15 for grad_head.  dz is rounded to half precision (2^-11 of its value at most); everything else is float32.
 // float32 operands are carried as two terms hi + lo (22 bits); a product of two of them is three, hi hi + lo hi + hi lo,
 // laid out as one contraction three times as long: [hi | lo | hi] against [hi | hi | lo].
 //
@@ -36,243 +36,330 @@ struct RowTargets {
   int k, groups;
 };
 
-__device__ __forceinline__ float block_max(float v, float* red) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
-__device__ __forceinline__ float block_sum(float v, float* red) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
-}
-
 template <class T> struct Vec;
 template <> struct Vec<float> { typedef f32x4 type; static constexpr int n = 4; };
 template <> struct Vec<bf16> { typedef bf16x8 type; static constexpr int n = 8; };
 
-// The exponent e for which |x| * 2^e lies in [2^13, 2^14), within what leaves 2^e and 2^-e finite; 0 for 0 and what is not finite.
+// The exponent e for which |x| * 2^e lies in [2^13, 2^14), within [-60, 60]; 0 for 0 and what is not finite.
 __device__ __forceinline__ int scale_exponent(float x) {
   if (!(x > 0.f) || x == INFINITY) return 0;
   int e;
   (void)frexpf(x, &e);                     // x = f 2^e, f in [1/2, 1)
-  return max(-100, min(100, 14 - e));
+  return max(-60, min(60, 14 - e));
 }
 
-struct PrepOut {
-  float *z_scale, *h_scale, *coef, *t_max;     // [T]; coef = g / tau and t_max = max |g h / tau| with a gradient only
-  int32_t* label;
-  int32_t* ids;
-  float *p, *ent, *mass;                       // lists; sum p log p and sum p of a row
+// The head where it is not read as it is: 64 x 64 elements of src [R, C] by 256 threads, as rows (F [Rp, Cp], contraction over
+// the columns) and transposed (FT [Cp, Rp], or nullptr), zeros past R and C.  TERMS 3: [hi | hi | lo], a third of the contraction
+// each.
+template <class T>
+struct HeadPack {
+  const T* src;
+  int64_t ld;
+  int R, C, Rp, Cp;
+  f16 *F, *FT;
+};
+template <class T, int TERMS>
+__device__ __forceinline__ void pack_tile(const HeadPack<T>& h, int tile_id, int t, float (&tile)[64][65]) {
+  const int across = h.Cp / 64, r0 = tile_id / across * 64, c0 = tile_id % across * 64;    // (r0 >= Rp: nothing)
+  const int r = r0 + (t >> 2), c = c0 + (t & 3) * 16;
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; i += Vec<T>::n) {
+    typename Vec<T>::type x;
+    const bool in = r < h.R && c + i < h.C;
+    if (in) x = *(const typename Vec<T>::type*)(h.src + (size_t)r * h.ld + c + i);
+#pragma unroll
+    for (int j = 0; j < Vec<T>::n; ++j) v[i + j] = in ? (float)x[j] * kWeightScale : 0.f;
+  }
+  auto put = [&](f16* dst, int m, int kk, int third, const float* x) {      // 8 elements of a row, from k kk on
+    f16x8 hi;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) hi[j] = from_f32<f16>(x[j]);
+    *(f16x8*)(dst + act_index(m, kk, TERMS * third)) = hi;
+    if constexpr (TERMS == 3) {
+      f16x8 lo;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) lo[j] = from_f32<f16>(x[j] - (float)hi[j]);
+      *(f16x8*)(dst + act_index(m, third + kk, 3 * third)) = hi;
+      *(f16x8*)(dst + act_index(m, 2 * third + kk, 3 * third)) = lo;
+    }
+  };
+  if (r < h.Rp) {
+    put(h.F, r, c, h.Cp, v);
+    put(h.F, r, c + 8, h.Cp, v + 8);
+  }
+  if (h.FT) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) tile[t >> 2][(t & 3) * 16 + j] = v[j];
+    __syncthreads();
+    const int col = t & 63, rr = (t >> 6) * 16;
+    if (r0 + rr < h.Rp) {
+      float x[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = tile[rr + j][col];
+      put(h.FT, c0 + col, r0 + rr, h.Rp, x);
+      put(h.FT, c0 + col, r0 + rr + 8, h.Rp, x + 8);
+    }
+  }
+}
+template <class T, int TERMS>
+__global__ __launch_bounds__(256) void loss_pack_kernel(HeadPack<T> head) {
+  __shared__ float tile[64][65];
+  pack_tile<T, TERMS>(head, blockIdx.x, threadIdx.x, tile);
+}
+
+struct RowsOut {
+  float *z_scale, *coef, *dz_coef, *dz_max;    // [T], with a gradient also g / tau, that over the row's scale, [Tp / 8] maxima of it
+  int32_t* label;                              // labels, -1 where there is no target
+  int32_t* ids;                                // lists; sum p log p and sum p of a row
+  float *p, *ent, *mass;
   unsigned short* first;
+  f16 *F, *FT;                                 // h in fragment order: rows [Tp, dP], and transposed [dP, Tp] (or nullptr)
 };
 
-// One workgroup a row: its target, and the scales of its h.
-template <class T>
-__global__ __launch_bounds__(256) void loss_prep_kernel(const T* __restrict__ h, int64_t ld, int d, int V, float inv_tau,
+// Eight rows a workgroup, a wave each: the row's target and scale, then its h as operands.  The workgroups behind those of the
+// rows pack the head (two tiles each), where a call packs it in one piece: a launch less.
+constexpr int kRowsChunk = 1024;               // columns at a time
+template <class T, int TERMS>
+__global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h, int64_t ld, int Tn, int d, int V, float inv_tau,
                                                         const int32_t* __restrict__ labels, const float* __restrict__ top_logits,
                                                         const int32_t* __restrict__ top_ids, int k, int groups,
-                                                        const float* __restrict__ g, PrepOut out) {
-  __shared__ float red[4], s_p[kMaxTop];
-  __shared__ int32_t s_id[kMaxTop], s_sorted[kMaxTop];
-  __shared__ unsigned char s_lead[kMaxTop];
-  __shared__ int s_n;
-  const int row = blockIdx.x, t = threadIdx.x;
-  bool live;
-  if (labels) {
+                                                        const float* __restrict__ g, int Tp, int dP, RowsOut out,
+                                                        HeadPack<T> head) {
+  constexpr int PITCH = kRowsChunk + 8;
+  __shared__ union {
+    __attribute__((aligned(16))) f16 row[TERMS == 3 ? 2 : 1][8 * PITCH];
+    float head[2][64][65];
+  } s_tile;
+  __shared__ float s_max[8];
+  if ((int)blockIdx.x >= Tp / 8) {
+    const int half = threadIdx.x >> 8;
+    pack_tile<T, TERMS>(head, ((int)blockIdx.x - Tp / 8) * 2 + half, threadIdx.x & 255, s_tile.head[half]);
+    return;
+  }
+  auto& tile = s_tile.row;
+  extern __shared__ __attribute__((aligned(16))) int32_t lists[];     // [8 rows][ids | keys | p], kp entries each
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = blockIdx.x * 8, row = row0 + wave;
+  bool live = row < Tn;
+  if (!live) {
+  } else if (labels) {
     const int32_t y = labels[row];
     live = y >= 0 && y < V;
-    if (t == 0) out.label[row] = live ? y : -1;
+    if (lane == 0) out.label[row] = live ? y : -1;
   } else {
-    if (t == 0) s_n = 0;
+    const int kp = (k + 3) & ~3;
+    int32_t *s_id = lists + wave * 3 * kp, *s_key = s_id + kp;
+    float* s_p = (float*)(s_key + kp);
     float m = -INFINITY;
-    for (int j = t; j < k; j += 256) {
-      const int32_t id = top_ids[(size_t)row * k + j];
-      const float l = top_logits[(size_t)row * k + j] * inv_tau;
-      const bool in = id >= 0 && id < V && l != -INFINITY;
-      s_id[j] = in ? id : -1;
+    for (int j = lane; j < kp; j += 64) {
+      int32_t id = -1;
+      float l = 0.f;
+      if (j < k) {
+        id = top_ids[(size_t)row * k + j];
+        l = top_logits[(size_t)row * k + j] * inv_tau;
+        if (id < 0 || id >= V || l == -INFINITY) id = -1;
+      }
+      s_id[j] = id;
       s_p[j] = l;
-      if (in) m = fmaxf(m, l);
+      if (id >= 0) m = fmaxf(m, l);
     }
-    m = block_max(m, red);
+    m = wave_max(m);
     m = m == -INFINITY ? 0.f : m;                                    // (all NaN, or none)
     float sum = 0.f;
-    for (int j = t; j < k; j += 256) {
+    for (int j = lane; j < kp; j += 64) {
       const float e = s_id[j] >= 0 ? expf(s_p[j] - m) : 0.f;
       s_p[j] = e;
       sum += e;
     }
-    sum = block_sum(sum, red);                                       // (its barriers publish s_id and s_p)
-    // equal ids: the first of them stands for all; its place is the number of smaller ids that stand
-    for (int j = t; j < k; j += 256) {
-      bool lead = s_id[j] >= 0;
-      for (int i = 0; lead && i < j; ++i) lead = s_id[i] != s_id[j];
-      s_lead[j] = lead;
+    sum = wave_sum(sum);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    // equal ids: the first of them stands for all, with its id as key; its place is the number of smaller keys
+    typedef __attribute__((ext_vector_type(4))) int i32x4;
+    constexpr int kNone = 0x7fffffff;
+    for (int j = lane; j < kp; j += 64) {
+      const int id = s_id[j];
+      bool lead = id >= 0;
+      for (int i = 0; i < kp; i += 4) {
+        const i32x4 o = *(const i32x4*)(s_id + i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) lead = lead && !(o[u] == id && i + u < j);
+      }
+      s_key[j] = lead ? id : kNone;
     }
-    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_wave_barrier();
     float ent = 0.f, mass = 0.f;
     int n = 0;
-    for (int j = t; j < k; j += 256)
-      if (s_lead[j]) {
-        const int32_t id = s_id[j];
-        int at = 0;
-        float p = 0.f;
-        for (int i = 0; i < k; ++i) {
-          if (s_lead[i] && s_id[i] < id) ++at;
-          if (s_id[i] == id) p += s_p[i];
+    for (int j = lane; j < kp; j += 64) {
+      const int id = s_key[j];
+      int at = 0;
+      float p = 0.f;
+      for (int i = 0; i < kp; i += 4) {
+        const i32x4 o = *(const i32x4*)(s_id + i), ky = *(const i32x4*)(s_key + i);
+        const f32x4 e = *(const f32x4*)(s_p + i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          at += ky[u] < id;
+          p += o[u] == id ? e[u] : 0.f;
         }
+      }
+      if (id != kNone) {
         p /= sum;
-        s_sorted[at] = id;
         out.ids[(size_t)row * k + at] = id;
         out.p[(size_t)row * k + at] = p;
         if (p != 0.f) ent += p * logf(p);
         mass += p;
         ++n;
       }
-    if (n) atomicAdd(&s_n, n);
-    ent = block_sum(ent, red);
-    mass = block_sum(mass, red);
-    n = s_n;
+    }
+    ent = wave_sum(ent);
+    mass = wave_sum(mass);
+    n = (int)wave_sum((float)n);
     live = n > 0;
-    if (t == 0) {
+    if (lane == 0) {
       out.ent[row] = ent;
       out.mass[row] = mass;
     }
-    for (int j = t; j <= groups; j += 256) {                         // first entry of id 64 j and more
-      int lo = 0, hi = n;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (s_sorted[mid] < j * kGroup) lo = mid + 1;
-        else hi = mid;
+    for (int b = lane; b <= groups; b += 64) {                       // first entry of id 64 b and more
+      int at = 0;
+      for (int i = 0; i < kp; i += 4) {
+        const i32x4 ky = *(const i32x4*)(s_key + i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) at += ky[u] < b * kGroup;
       }
-      out.first[(size_t)row * (groups + 1) + j] = (unsigned short)lo;
+      out.first[(size_t)row * (groups + 1) + b] = (unsigned short)at;
     }
   }
+  const T* x = h + (size_t)row * ld;
   float mx = 0.f;
-  if (live) {
-    const T* x = h + (size_t)row * ld;
-    for (int i = t * Vec<T>::n; i < d; i += 256 * Vec<T>::n) {
+  if (live)
+    for (int i = lane * Vec<T>::n; i < d; i += 64 * Vec<T>::n) {
       const typename Vec<T>::type v = *(const typename Vec<T>::type*)(x + i);
 #pragma unroll
       for (int j = 0; j < Vec<T>::n; ++j) mx = fmaxf(mx, fabsf((float)v[j]));
     }
-  }
-  mx = block_max(mx, red);
-  if (t == 0) {
-    const int e = live ? scale_exponent(mx) : 0;
-    out.h_scale[row] = live ? ldexpf(1.0f, e) : 0.f;
+  mx = wave_max(mx);
+  const int e = live ? scale_exponent(mx) : 0;
+  const float scale = live ? ldexpf(1.0f, e) : 0.f;
+  float top = 0.f;
+  if (lane == 0 && row < Tn) {
     out.z_scale[row] = live ? ldexpf(inv_tau / kWeightScale, -e) : 0.f;
     if (g) {
-      const float c = live ? g[row] * inv_tau : 0.f;
+      const float c = live ? g[row] * inv_tau : 0.f, s = ldexpf(c, -e);
       out.coef[row] = c;
-      out.t_max[row] = fabsf(c) * mx;
+      out.dz_coef[row] = s;
+      top = fabsf(s) < INFINITY ? fabsf(s) : 0.f;
     }
+  }
+  if (lane == 0) s_max[wave] = top;
+  __syncthreads();
+  if (g && threadIdx.x == 0) {
+    float t = s_max[0];
+    for (int i = 1; i < 8; ++i) t = fmaxf(t, s_max[i]);
+    out.dz_max[blockIdx.x] = t;
+  }
+  for (int c0 = 0; c0 < dP; c0 += kRowsChunk) {
+    const int n = min(kRowsChunk, dP - c0);
+    if (c0) __syncthreads();
+    for (int i = lane * Vec<T>::n; i < n; i += 64 * Vec<T>::n) {
+      typename Vec<T>::type v;
+      const bool in = live && c0 + i < d;
+      if (in) v = *(const typename Vec<T>::type*)(x + c0 + i);
+#pragma unroll
+      for (int j = 0; j < Vec<T>::n; ++j) {
+        const float y = in ? (float)v[j] * scale : 0.f;
+        const f16 hi = from_f32<f16>(y);
+        tile[0][wave * PITCH + i + j] = hi;
+        if constexpr (TERMS == 3) tile[1][wave * PITCH + i + j] = from_f32<f16>(y - (float)hi);
+      }
+    }
+    __syncthreads();
+    const int ldF = TERMS * dP, ldT = TERMS * Tp;
+    for (int i = threadIdx.x; i < n; i += 512) {                     // rows: 8 of a chunk of 8 columns side by side
+      const int r = i & 7, c = i & ~7;
+      const f16x8 hi = *(const f16x8*)(&tile[0][r * PITCH + c]);
+      *(f16x8*)(out.F + act_index(row0 + r, c0 + c, ldF)) = hi;
+      if constexpr (TERMS == 3) {
+        *(f16x8*)(out.F + act_index(row0 + r, dP + c0 + c, ldF)) = *(const f16x8*)(&tile[TERMS == 3][r * PITCH + c]);
+        *(f16x8*)(out.F + act_index(row0 + r, 2 * dP + c0 + c, ldF)) = hi;
+      }
+    }
+    if (out.FT)
+      for (int i = threadIdx.x; i < n; i += 512) {                   // columns: their 8 rows
+        f16x8 hi, lo;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          hi[r] = tile[0][r * PITCH + i];
+          if constexpr (TERMS == 3) lo[r] = tile[TERMS == 3][r * PITCH + i];
+        }
+        *(f16x8*)(out.FT + act_index(c0 + i, row0, ldT)) = hi;
+        if constexpr (TERMS == 3) {
+          *(f16x8*)(out.FT + act_index(c0 + i, Tp + row0, ldT)) = hi;
+          *(f16x8*)(out.FT + act_index(c0 + i, 2 * Tp + row0, ldT)) = lo;
+        }
+      }
   }
 }
 
-// The power of two for g h / tau as one tensor: out[0], and its inverse times those of dz: out[1].
-__global__ __launch_bounds__(256) void loss_scale_kernel(const float* __restrict__ t_max, int T, float* __restrict__ out) {
+// The largest of n values to the first of them (a launch of its own for what every wave of the products would have to read).
+__global__ __launch_bounds__(256) void loss_max_kernel(float* __restrict__ v, int n) {
   __shared__ float red[4];
   float m = 0.f;
-  for (int i = threadIdx.x; i < T; i += 256) m = t_max[i] < INFINITY ? fmaxf(m, t_max[i]) : m;
-  m = block_max(m, red);
-  if (threadIdx.x == 0) {
-    const int e = scale_exponent(m);
-    out[0] = ldexpf(1.0f, e);
-    out[1] = ldexpf(1.0f / kDzScale, -e);
-  }
+  for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, v[i]);
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) v[0] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+// 2^x that brings the largest of n values into [1/2, 1); the same in every wave.
+__device__ __forceinline__ int max_exponent(const float* v, int n, int lane) {
+  float m = 0.f;
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, v[i]);
+  m = wave_max(m);
+  if (!(m > 0.f)) return 0;
+  int e;
+  (void)frexpf(m, &e);
+  return max(-120, min(120, -e));
 }
 
 // ---- operands in fragment order ---------------------------------------------------------------------------------
-// 64 x 64 elements of src [R, C] a workgroup: as rows (F, ld halves a row, contraction over the columns) and / or transposed (FT,
-// contraction over the rows), zeros past R and C up to Rp and Cp.  TERMS 3: [hi | lo | hi] (B: [hi | hi | lo]), a third of the
-// contraction each.  f_scale, ft_scale: [R] or nullptr; rows of f_scale 0 are zero whatever they hold.
-template <class T, int TERMS, bool B>
-__global__ __launch_bounds__(256) void loss_pack_kernel(const T* __restrict__ src, int64_t ld_src, int R, int C, int Rp, int Cp,
-                                                        float scale, const float* __restrict__ f_scale,
-                                                        const float* __restrict__ ft_row, const float* __restrict__ ft_all,
-                                                        f16* __restrict__ F, f16* __restrict__ FT) {
-  __shared__ float tile[64][65];
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, t = threadIdx.x;
-  const int r = r0 + (t >> 2), c = c0 + (t & 3) * 16;
-  float v[16];
-  const float fs = f_scale ? (r < R ? f_scale[r] : 0.f) : scale;
-  const bool live = r < R && fs != 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; i += Vec<T>::n) {
-    typename Vec<T>::type x;
-    const bool in = live && c + i < C;
-    if (in) x = *(const typename Vec<T>::type*)(src + (size_t)r * ld_src + c + i);
-#pragma unroll
-    for (int j = 0; j < Vec<T>::n; ++j) v[i + j] = in ? (float)x[j] : 0.f;
-  }
-  // 8 elements of a row, from k kk on.  What half precision does not hold becomes a NaN: an infinite head row would make a logit
-  // of -inf, which a softmax takes for a probability of 0.
-  auto put = [&](f16* dst, int m, int kk, int third, const float* x) {
-    f16x8 hi;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) hi[j] = fabsf(x[j]) <= 65504.0f ? from_f32<f16>(x[j]) : (f16)NAN;
-    *(f16x8*)(dst + act_index(m, kk, TERMS * third)) = hi;
-    if constexpr (TERMS == 3) {
-      f16x8 lo;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) lo[j] = from_f32<f16>(x[j] - (float)hi[j]);
-      *(f16x8*)(dst + act_index(m, third + kk, 3 * third)) = B ? hi : lo;
-      *(f16x8*)(dst + act_index(m, 2 * third + kk, 3 * third)) = B ? lo : hi;
-    }
-  };
-  if (F && r < Rp && c < Cp) {
-    float x[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = v[j] * fs;
-    put(F, r, c, Cp, x);
-    put(F, r, c + 8, Cp, x + 8);
-  }
-  if (FT) {
-    float s = scale;
-    if (ft_row) s = r < R ? ft_row[r] : 0.f;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) tile[t >> 2][(t & 3) * 16 + j] = live ? v[j] * s : 0.f;
-    __syncthreads();
-    const float all = ft_all ? ft_all[0] : 1.0f;
-    const int col = t & 63, rr = (t >> 6) * 16;
-    if (c0 + col < Cp && r0 + rr < Rp) {
-      float x[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) x[j] = tile[rr + j][col] * all;
-      put(FT, c0 + col, r0 + rr, Rp, x);
-      put(FT, c0 + col, r0 + rr + 8, Rp, x + 8);
-    }
-  }
-}
-
 // ---- epilogues -----------------------------------------------------------------------------------------------
+// z of an accumulated product.  An infinite weight makes an infinite product, which as -inf would count as a probability of 0:
+// anything infinite becomes a NaN.
+__device__ __forceinline__ float to_z(float x, float z_scale) { return fmaf(x, 0.f, x) * z_scale; }
+
 // Partial statistics of the groups of 64 columns.  ROWS rows of a group by 64 / ROWS lanes each; a group's sums are formed in
 // the same order whatever the tile, so a row's loss does not depend on the rows beside it.
+template <int RAW>
 struct EpiStats {
-  static constexpr int kSpan = 64;
+  static constexpr int kSpan = 64, kRaw = RAW;
   RowTargets tg;
-  float *pm, *pl, *pa;       // [groups][T]
+  float *pm, *pl;            // [groups][T]
+  float* pa;                 // z of the label [T], or p z of the entries [T][k]
   int T, V, n_base;          // first column of the launch
+  int64_t raw_ld;
+  int raw_rows;
   template <int COLS, int PITCH, int ROWS>
   __device__ __forceinline__ void consume(const float* tile, int m_base, int nb, int lane, int M) const {
     constexpr int PARTS = 64 / ROWS, W = kGroup / PARTS;
     static_assert(COLS % kGroup == 0 && W % 16 == 0 && W <= 32, "whole groups, sums of 16 or of two of them a lane");
     const int r = lane % ROWS, part = lane / ROWS, m = m_base + r, mc = min(m, M - 1);
     const float zs = tg.z_scale[mc];
+    const int label = tg.label ? tg.label[mc] : -1;
 #pragma unroll
     for (int gg = 0; gg < COLS / kGroup; ++gg) {
-      const int n0 = n_base + nb + gg * kGroup, c0 = gg * kGroup + part * W;
-      const float* x = tile + r * PITCH + c0;
+      const int n0 = n_base + nb + gg * kGroup, c0 = gg * kGroup + part * W, left = V - n0 - part * W;
+      float x[W];
+#pragma unroll
+      for (int i = 0; i < W; i += 4) *(f32x4*)(x + i) = *(const f32x4*)(tile + r * PITCH + c0 + i);
       float mx = -INFINITY;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const float z = x[i] * zs;
-        if (n0 + part * W + i < V) mx = fmaxf(mx, z);
+        x[i] = to_z(x[i], zs);
+        if (left < W) x[i] = i < left ? x[i] : -INFINITY;            // (uniform but for the lanes' parts)
+        mx = fmaxf(mx, x[i]);
       }
 #pragma unroll
       for (int s = ROWS; s < 64; s *= 2) mx = fmaxf(mx, __shfl_xor(mx, s, 64));
@@ -282,49 +369,53 @@ struct EpiStats {
       for (int h = 0; h < W / 16; ++h) {
         float s4[4] = {};
 #pragma unroll
-        for (int i = 16 * h; i < 16 * h + 16; ++i) {
-          const float e = __builtin_amdgcn_exp2f((x[i] * zs - ref) * kLog2e);
-          s4[i & 3] += n0 + part * W + i < V ? e : 0.f;
-        }
+        for (int i = 16 * h; i < 16 * h + 16; ++i) s4[i & 3] += __builtin_amdgcn_exp2f((x[i] - ref) * kLog2e);
         l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
       }
 #pragma unroll
       for (int s = ROWS; s < 64; s *= 2) l += __shfl_xor(l, s, 64);
-      if (part == 0 && m < M) {
-        float a = 0.f;
+      if (part == 0 && m < M && n0 < V) {
         if (tg.label) {
-          const int c = tg.label[m] - n0;
-          if (c >= 0 && c < kGroup) a = tile[r * PITCH + gg * kGroup + c] * zs;
+          const int c = label - n0;
+          if (c >= 0 && c < kGroup) pa[m] = to_z(tile[r * PITCH + gg * kGroup + c], zs);
         } else {
           const unsigned short* f = tg.first + (size_t)m * (tg.groups + 1) + n0 / kGroup;
-          for (int e = n0 < V ? f[0] : 0, end = n0 < V ? f[1] : 0; e < end; ++e)
-            a += tg.p[(size_t)m * tg.k + e] * (tile[r * PITCH + gg * kGroup + tg.ids[(size_t)m * tg.k + e] - n0] * zs);
+          for (int e = f[0], end = f[1]; e < end; ++e) {
+            const size_t at = (size_t)m * tg.k + e;
+            pa[at] = tg.p[at] * to_z(tile[r * PITCH + gg * kGroup + tg.ids[at] - n0], zs);
+          }
         }
-        if (n0 < V) {
-          const size_t at = (size_t)(n0 / kGroup) * T + m;
-          pm[at] = mx;
-          pl[at] = l;
-          pa[at] = a;
-        }
+        const size_t at = (size_t)(n0 / kGroup) * T + m;
+        pm[at] = mx;
+        pl[at] = l;
       }
     }
   }
 };
 
-// dz * 2^15 as the operand of both gradient products: rows (F) and transposed (FT).  Rows T .. Tp and columns V .. are zeros.
+// dz as the operand of both gradient products: rows (F, times 2^15) and transposed (FT, times the rows' coefficients and what
+// brings them all to 2^15).  Rows T .. Tp and columns V .. are zeros.
+template <int RAW, int TERMS>
 struct EpiDz {
-  static constexpr int kSpan = 64;
+  static constexpr int kSpan = 64, kRaw = RAW;
   RowTargets tg;
   const float* lse;
+  const float *dz_coef, *dz_max;
+  int n_max;
   f16 *F, *FT;
-  int Tp, Np, terms;         // Np: the launch's columns
+  int Tp, Np;                // Np: the launch's columns
   int V, n_base;
+  int64_t raw_ld;
+  int raw_rows;
+  float ft_scale;
+  __device__ __forceinline__ void begin(int lane) { ft_scale = ldexpf(kDzScale, max_exponent(dz_max, n_max, lane)); }
+  template <bool B>
   __device__ __forceinline__ void put(f16* dst, int m, int k, int third, const float (&x)[8]) const {
     f16x8 hi;
 #pragma unroll
     for (int j = 0; j < 8; ++j) hi[j] = from_f32<f16>(x[j]);
-    *(f16x8*)(dst + act_index(m, k, terms * third)) = hi;
-    if (terms == 3) {
+    *(f16x8*)(dst + act_index(m, k, TERMS * third)) = hi;
+    if constexpr (TERMS == 3) {
       f16x8 lo;
 #pragma unroll
       for (int j = 0; j < 8; ++j) lo[j] = from_f32<f16>(x[j] - (float)hi[j]);
@@ -337,7 +428,7 @@ struct EpiDz {
     float* tile = const_cast<float*>(tile_in);
     constexpr int PARTS = 64 / ROWS, CH = COLS / 8;
     const int r = lane % ROWS, part = lane / ROWS, m = m_base + r, mc = min(m, M - 1);
-    const float zs = m < M ? tg.z_scale[mc] : 0.f, ls = lse[mc];
+    const float zs = m < M ? tg.z_scale[mc] : 0.f, ls = lse[mc], ft = dz_coef[mc] * ft_scale;
     const int label = tg.label ? tg.label[mc] : -1;
 #pragma unroll
     for (int it = 0; it < CH / PARTS; ++it) {
@@ -346,9 +437,8 @@ struct EpiDz {
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float q = __builtin_amdgcn_exp2f((x[j] * zs - ls) * kLog2e);
-        if (n + j == label) q -= 1.0f;
-        v[j] = q;
+        const float q = __builtin_amdgcn_exp2f((to_z(x[j], zs) - ls) * kLog2e);
+        v[j] = n + j == label ? q - 1.0f : q;
       }
       if (!tg.label && zs != 0.f && n < V) {
         const unsigned short* f = tg.first + (size_t)m * (tg.groups + 1) + n / kGroup;
@@ -360,14 +450,19 @@ struct EpiDz {
         }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = zs != 0.f && n + j < V ? v[j] * kDzScale : 0.f;
-        x[j] = v[j];
+      for (int j = 0; j < 8; ++j) v[j] = zs != 0.f && n + j < V ? v[j] : 0.f;
+      if (FT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = zs != 0.f ? v[j] * ft : 0.f;
       }
-      if (F && m < Tp) put(F, m, nb + c, Np, v);
+      if (F && m < Tp) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= kDzScale;
+        put<false>(F, m, nb + c, Np, v);
+      }
     }
     if (FT) {
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
       __builtin_amdgcn_wave_barrier();
       constexpr int RC = ROWS / 8;                       // chunks of 8 rows
 #pragma unroll
@@ -376,137 +471,173 @@ struct EpiDz {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = tile[(rc * 8 + j) * PITCH + c];
-        if (m_base + rc * 8 < Tp) put(FT, nb + c, m_base + rc * 8, Tp, v);
+        if (m_base + rc * 8 < Tp) put<false>(FT, nb + c, m_base + rc * 8, Tp, v);
       }
       __builtin_amdgcn_wave_barrier();
     }
   }
 };
 
-// grad_hidden: the pieces' products summed in float32, the last one times g / tau and rounded.
+// Rounds four results to the storage type.
+__device__ __forceinline__ void store_result(void* out, size_t at, bool f32, const f32x4& g) {
+  if (f32) {
+    *(f32x4*)((float*)out + at) = g;
+  } else {
+    bf16x4 o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = from_f32<bf16>(g[j]);
+    *(bf16x4*)((bf16*)out + at) = o;
+  }
+}
+
+// grad_hidden of one slice of the vocabulary: a plane of float32 sums, or, where there is only one, the result.
+template <int RAW>
 struct EpiHidden {
-  static constexpr int kSpan = 64;
-  float* acc;                // [T][ld]
-  int ld;
-  int first, last;           // of the pieces
+  static constexpr int kSpan = 64, kRaw = RAW;
+  static constexpr bool kSliced = true;
+  int slices;
+  float* planes;             // [slices][T][ld], or nullptr
+  int add;                   // to what is there
+  int T, ld;
   const float* coef;
   void* out;
   int out_f32, d;
+  int64_t raw_ld;
+  int raw_rows, raw_cols;
+  __device__ __forceinline__ void slice(int kz) { if (planes) planes += (size_t)kz * T * ld; }
   template <int COLS, int PITCH, int ROWS>
   __device__ __forceinline__ void consume(const float* tile, int m_base, int nb, int lane, int M) const {
     constexpr int LPR = COLS / 4, RPI = 64 / LPR, IT = ROWS / RPI;
     const int r0 = lane / LPR, c4 = (lane % LPR) * 4;
-    f32x4 v[IT];
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-      v[it] = *(const f32x4*)(tile + (it * RPI + r0) * PITCH + c4) * (1.0f / (kDzScale * kWeightScale));
-      if (!first) v[it] += *(const f32x4*)(acc + (size_t)min(m_base + it * RPI + r0, M - 1) * ld + nb + c4);
-    }
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int m = m_base + it * RPI + r0;
-      if (m >= M) continue;
-      if (!last) {
-        *(f32x4*)(acc + (size_t)m * ld + nb + c4) = v[it];
-      } else if (nb + c4 < d) {
-        const f32x4 g = v[it] * coef[m];
-        const size_t at = (size_t)m * d + nb + c4;
-        if (out_f32) {
-          *(f32x4*)((float*)out + at) = g;
-        } else {
-          bf16x4 o;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = from_f32<bf16>(g[j]);
-          *(bf16x4*)((bf16*)out + at) = o;
-        }
+      const int r = it * RPI + r0, m = m_base + r;
+      const f32x4 v = *(const f32x4*)(tile + r * PITCH + c4) * (1.0f / (kDzScale * kWeightScale));
+      if (m >= M || nb + c4 >= d) continue;
+      if (planes) {
+        f32x4* p = (f32x4*)(planes + (size_t)m * ld + nb + c4);
+        *p = add ? *p + v : v;
+      } else {
+        store_result(out, (size_t)m * d + nb + c4, out_f32, v * coef[m]);
       }
     }
   }
 };
+// ... and the planes in their order.
+__global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restrict__ planes, int n, int T, int ld, int d,
+                                                          const float* __restrict__ coef, void* __restrict__ out, int out_f32) {
+  const int c = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, m = blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (m >= T || c >= d) return;
+  const size_t plane = (size_t)T * ld;
+  const float* p = planes + (size_t)m * ld + c;
+  f32x4 v = *(const f32x4*)p;
+  int i = 1;
+  for (; i + 3 < n; i += 4) {
+    f32x4 u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = *(const f32x4*)(p + (i + j) * plane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v += u[j];
+  }
+  for (; i < n; ++i) v += *(const f32x4*)(p + i * plane);
+  store_result(out, (size_t)m * d + c, out_f32, v * coef[m]);
+}
 
 // grad_head: rows of a piece of the vocabulary.
 struct EpiHead {
   static constexpr int kSpan = 64;
   void* out;                 // the piece's first row
   int out_f32, d, rows;
-  const float* scale;        // [1]
+  const float* dz_max;
+  int n_max;
+  float scale;
+  __device__ __forceinline__ void begin(int lane) { scale = ldexpf(1.0f / kDzScale, -max_exponent(dz_max, n_max, lane)); }
   template <int COLS, int PITCH, int ROWS>
   __device__ __forceinline__ void consume(const float* tile, int m_base, int nb, int lane, int M) const {
     constexpr int LPR = COLS / 4, RPI = 64 / LPR, IT = ROWS / RPI;
     const int r0 = lane / LPR, c4 = (lane % LPR) * 4;
-    const float s = scale[1];
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int r = it * RPI + r0, m = m_base + r;
-      const f32x4 g = *(const f32x4*)(tile + r * PITCH + c4) * s;
-      if (m >= rows || nb + c4 >= d) continue;
-      const size_t at = (size_t)m * d + nb + c4;
-      if (out_f32) {
-        *(f32x4*)((float*)out + at) = g;
-      } else {
-        bf16x4 o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = from_f32<bf16>(g[j]);
-        *(bf16x4*)((bf16*)out + at) = o;
-      }
+      const f32x4 g = *(const f32x4*)(tile + r * PITCH + c4) * scale;
+      if (m < rows && nb + c4 < d) store_result(out, (size_t)m * d + nb + c4, out_f32, g);
     }
   }
 };
 
+static int round_up(int x, int n) { return (x + n - 1) / n * n; }
+static int tile_up(int x) { return x <= 128 ? 128 : round_up(x, 256); }        // columns of a product
+
 // The tiles of gemm_f16_variant, of which those of 64x256, 160x256 and 224x256 are run as their neighbours: EpiDz writes whole
 // blocks of 64 rows, and the difference does not pay for another instance each.
 template <class Epi>
-static void product(const f16* A, const f16* W, int M, int N, int K, const Epi& epi, hipStream_t st) {
-  const GemmF16 g{A, K, W, M, N, K, K, nullptr};
-  constexpr bool four = std::is_same_v<Epi, EpiHidden> || std::is_same_v<Epi, EpiHead>;    // 128x128 waves, as residual adds
-  switch (gemm_f16_variant(M, N, K, K, false, Epi::kSpan)) {
+static void product(const f16* A, int lda, const void* W, int M, int N, int K, const Epi& epi, hipStream_t st) {
+  const GemmF16 g{A, lda, (const f16*)W, M, N, K, K, nullptr};
+  constexpr bool four = std::is_same_v<Epi, EpiHidden<0>> || std::is_same_v<Epi, EpiHead>;    // 128x128 waves, as residual adds
+  int n = N, k = K;
+  if constexpr (sliced<Epi>()) n = N * epi.slices, k = round_up(K / epi.slices, PK);          // (as in hidden_slices)
+  int variant = gemm_f16_variant(M, n, k, k, false, Epi::kSpan);
+  switch (variant) {
     case V_64x128_8W: launch<2, 4, 32, 32, 4, 4, 1, true, false, false>(g, epi, st); break;
     case V_64x128: case V_64x128_ROUNDS: launch<2, 2, 32, 64, 3, 3, 2, false, false, false>(g, epi, st); break;
     case V_128x128: launch<4, 2, 32, 64, 4, 4, 1, false, false, false>(g, epi, st); break;
     case V_64x256: case V_128x256: launch<2, 4, 64, 64, 3, 3, 1, false, false, false>(g, epi, st); break;
     case V_160x256: case V_192x256: launch<2, 4, 96, 64, 2, 3, 1, false, false, false>(g, epi, st); break;
     default:
-      if constexpr (four) launch<2, 2, 128, 128, 2, 3, 1, false, true, false>(g, epi, st);
+      if constexpr (raw_w<Epi>() != 0) launch<2, 4, 96, 64, 2, 3, 1, false, false, false>(g, epi, st);      // (registers)
+      else if constexpr (four) launch<2, 2, 128, 128, 2, 3, 1, false, true, false>(g, epi, st);
       else launch<4, 2, 64, 128, 2, 3, 1, false, true, false>(g, epi, st);
   }
 }
 
 // ---- joining the groups -------------------------------------------------------------------------------------------
-// 16 rows a workgroup, 16 lanes a row; a lane takes every 16th group, and the lanes are joined in their order.
-__global__ __launch_bounds__(256) void loss_join_kernel(const float* __restrict__ pm, const float* __restrict__ pl,
-                                                        const float* __restrict__ pa, int T, int groups, RowTargets tg,
-                                                        const float* __restrict__ ent, const float* __restrict__ mass,
-                                                        float* __restrict__ loss, float* __restrict__ lse) {
-  __shared__ float sm[16][17], sl[16][17], sa[16][17];
+// 16 rows a workgroup, 64 threads a row, which take every 64th group; their sums are joined in a tree.
+__global__ __launch_bounds__(1024) void loss_join_kernel(const float* __restrict__ pm, const float* __restrict__ pl,
+                                                         const float* __restrict__ pa, int T, int groups, RowTargets tg,
+                                                         const float* __restrict__ ent, const float* __restrict__ mass,
+                                                         float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float sm[64][17], sl[64][17], sa[64][17];
   const int r = threadIdx.x & 15, part = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
+  const bool live = row < T && tg.z_scale[row] != 0.f;
   float m = -INFINITY, l = 0.f, a = 0.f;
-  if (row < T) {
-    for (int g = part; g < groups; g += 16) m = fmaxf(m, pm[(size_t)g * T + row]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    for (int g = part; g < groups; g += 16) {
-      const size_t at = (size_t)g * T + row;
-      l += pl[at] * __builtin_amdgcn_exp2f((pm[at] - ref) * kLog2e);
-      a += pa[at];
+  auto add = [](float& m, float& l, float m2, float l2) {            // (m, l) and another one to a common maximum
+    const float mm = fmaxf(m, m2), ref = mm == -INFINITY ? 0.f : mm;
+    l = l * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + l2 * __builtin_amdgcn_exp2f((m2 - ref) * kLog2e);
+    m = mm;
+  };
+  if (live) {
+    for (int g0 = part; g0 < groups; g0 += 256) {
+      float um[4], ul[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const size_t at = (size_t)min(g0 + 64 * u, groups - 1) * T + row;
+        um[u] = pm[at];
+        ul[u] = pl[at];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (g0 + 64 * u < groups) add(m, l, um[u], ul[u]);
     }
+    if (!tg.label)
+      for (int e = part, n = tg.first[(size_t)row * (groups + 1) + groups]; e < n; e += 64) a += pa[(size_t)row * tg.k + e];
   }
   sm[part][r] = m;
   sl[part][r] = l;
   sa[part][r] = a;
-  __syncthreads();
-  if (part == 0 && row < T) {
-    float mm = -INFINITY;
-    for (int i = 0; i < 16; ++i) mm = fmaxf(mm, sm[i][r]);
-    const float ref = mm == -INFINITY ? 0.f : mm;
-    l = a = 0.f;
-    for (int i = 0; i < 16; ++i) {
-      const float mi = sm[i][r] == -INFINITY ? 0.f : sm[i][r];
-      l += sl[i][r] * __builtin_amdgcn_exp2f((mi - ref) * kLog2e);
-      a += sa[i][r];
+  for (int s = 32; s > 0; s >>= 1) {
+    __syncthreads();
+    if (part < s) {
+      add(m, l, sm[part + s][r], sl[part + s][r]);
+      a += sa[part + s][r];
+      sm[part][r] = m;
+      sl[part][r] = l;
+      sa[part][r] = a;
     }
-    const bool live = tg.z_scale[row] != 0.f;
-    const float n = ref + logf(l);
+  }
+  if (part == 0 && row < T) {
+    const float n = (m == -INFINITY ? 0.f : m) + logf(l);
     lse[row] = live ? n : 0.f;
-    loss[row] = !live ? 0.f : tg.label ? n - a : ent[row] + mass[row] * n - a;
+    if (loss) loss[row] = !live ? 0.f : tg.label ? n - pa[row] : ent[row] + mass[row] * n - a;
   }
 }
 
@@ -516,13 +647,36 @@ namespace {
 struct Plan {
   int T, d, V, k, terms, groups;
   int Tp, dP, Vp;              // padded sizes of operands: contractions in whole slabs, columns in whole tiles
-  int piece;                   // columns of the vocabulary at a time (gradient)
-  size_t z_scale, h_scale, coef, t_max, scales, label, ids, p, ent, mass, first;
-  size_t hF, hT, wF, wT, dzF, dzT, acc, pm, pl, pa, bytes;
+  bool raw;                    // the head is read as it is
+  int piece, pieces;           // columns of the vocabulary at a time (gradient)
+  int slices;                  // of a piece, for grad_hidden, whose sums are in planes: of each slice, of up to four pieces
+  int sets;                    // (later pieces add to the planes of earlier ones)
+  size_t z_scale, coef, dz_coef, dz_max, label, ids, p, ent, mass, first;
+  size_t hF, hT, wF, wT, dzF, dzT, planes, pm, pl, pa, lse, bytes;
 };
 
-int round_up(int x, int n) { return (x + n - 1) / n * n; }
-int tile_up(int x) { return x <= 128 ? 128 : round_up(x, 256); }        // columns of a product
+// Slices of the contraction over K of grad_hidden: the number that the model of a launch's time, with the columns of all
+// slices beside one another, and the planes' bytes (written and read, 4 TB/s) make cheapest.
+int hidden_slices(int T, int dP, int K) {
+  int best = 1;
+  float best_us = gemm_f16_model_us(T, dP, K);
+  for (int s = 2; s <= K / PK / 4 && s <= 64; s += s < 8 ? 1 : s < 16 ? 2 : 4) {
+    const float us = gemm_f16_model_us(T, dP * s, round_up(K / s, PK)) + 3.0f + (float)s * T * dP * 8e-6f / 4.0f;
+    if (us < best_us) best_us = us, best = s;
+  }
+  return best;
+}
+
+// A bfloat16 head is read as it is where packing it (5 TB/s of twice its bytes, three times with a gradient) costs more than what
+// the products lose by re-encoding it between the LDS and the matrix cores (a third of their rate where they bound).  us, as it
+// is / packed, loss and gradient: 32000 x 4096 56 rows 57 / 148, 238 / 365, 384 rows 112 / 185, 425 / 525, 768 rows 202 / 258, 653 / 728,
+// 1536 rows 404 / 391, 1196 / 1148; 32000 x 768 56 rows 21 / 34, 54 / 73, 256 rows 31 / 39, 92 / 96, 512 rows 57 / 50, 160 / 133;
+// 8000 x 2048 256 rows 30 / 31, 70 / 71, 384 rows 45 / 35, 101 / 84; 2000 x 4096 one row 41 / 31, 56 / 52; 4000 x 1024 the same
+// within 5 % up to 384 rows.
+bool reads_head_as_it_is(int T, int d, int V) {
+  const long long size = (long long)d * V, least = 12'000'000;
+  return size >= least && T <= 256 + (size - least) / 256'000;
+}
 
 Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   Plan w{};
@@ -530,18 +684,22 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   w.terms = r.dtype == VLA_F32 ? 3 : 1;
   w.Tp = round_up(w.T, 64), w.dP = tile_up(w.d), w.Vp = tile_up(w.V);
   w.groups = (w.V + kGroup - 1) / kGroup;
+  w.raw = r.dtype == VLA_BF16 && w.d % PK == 0 && reads_head_as_it_is(w.T, w.d, w.V);
   const size_t half = 2 * (size_t)w.terms;
-  w.piece = w.Vp;
-  if (grad) {                                                       // dz, both ways, within 256 MB
-    const size_t cols = (((size_t)256 << 20) / (2 * half * w.Tp)) & ~(size_t)255;
+  w.piece = w.Vp, w.pieces = w.slices = 1;
+  if (grad) {                                                       // dz, both ways, within 512 MB
+    const size_t cols = (((size_t)512 << 20) / (2 * half * w.Tp)) & ~(size_t)255;
     const int most = cols < 256 ? 256 : cols > (size_t)w.Vp ? w.Vp : (int)cols;
-    const int n = (w.Vp + most - 1) / most;
-    w.piece = n == 1 ? w.Vp : round_up((w.Vp + n - 1) / n, 256);
+    w.pieces = (w.Vp + most - 1) / most;
+    w.piece = w.pieces == 1 ? w.Vp : round_up((w.Vp + w.pieces - 1) / w.pieces, 256);
+    w.pieces = (w.Vp + w.piece - 1) / w.piece;
+    // (a slab at least in every slice of the last piece)
+    w.slices = min(hidden_slices(w.T, w.dP, w.terms * w.piece), (w.V - (w.pieces - 1) * w.piece + PK - 1) / PK);
   }
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
   const size_t T = (size_t)w.T;
-  w.z_scale = take(4 * T), w.h_scale = take(4 * T);
+  w.z_scale = take(4 * T);
   if (k) {
     w.ids = take(4 * T * k), w.p = take(4 * T * k), w.ent = take(4 * T), w.mass = take(4 * T);
     w.first = take(2 * T * (w.groups + 1));
@@ -549,15 +707,16 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
     w.label = take(4 * T);
   }
   w.hF = take((size_t)w.Tp * w.dP * half);
-  w.wF = take((size_t)w.piece * w.dP * half);
+  if (!w.raw) w.wF = take((size_t)w.piece * w.dP * half);
+  if (!grad || w.terms == 3) w.pm = take(4 * T * w.groups), w.pl = take(4 * T * w.groups), w.pa = take(4 * T * (k ? k : 1));
   if (grad) {
-    w.coef = take(4 * T), w.t_max = take(4 * T), w.scales = take(8);
+    w.coef = take(4 * T), w.dz_coef = take(4 * T), w.dz_max = take(w.Tp / 2);
     w.hT = take((size_t)w.Tp * w.dP * half);
-    w.wT = take((size_t)w.piece * w.dP * half);
+    if (!w.raw) w.wT = take((size_t)w.piece * w.dP * half);
     w.dzF = take((size_t)w.Tp * w.piece * half), w.dzT = take((size_t)w.Tp * w.piece * half);
-    if (w.piece < w.Vp) w.acc = take(4 * T * w.dP);
-  } else {
-    w.pm = take(4 * T * w.groups), w.pl = take(4 * T * w.groups), w.pa = take(4 * T * w.groups);
+    w.sets = min(w.pieces, 4);
+    if (w.sets * w.slices > 1) w.planes = take(4 * T * w.dP * w.sets * w.slices);
+    if (w.terms == 3) w.lse = take(4 * T);
   }
   w.bytes = at;
   return w;
@@ -572,7 +731,7 @@ int check_rows(const vla_head_rows* r, bool pointers) {
   if (!(r->temperature >= 0.f) || r->temperature > 3e38f) return VLA_E_SHAPE;
   if (!pointers) return VLA_OK;
   if (!r->hidden || !r->head) return VLA_E_NULL;
-  if (r->ld_hidden < r->d_model || r->ld_head < r->d_model || r->ld_hidden % unit || r->ld_head % unit) return VLA_E_SHAPE;
+  if (r->ld_hidden < r->d_model || r->ld_head < r->d_model || r->ld_hidden > 1 << 22 || r->ld_head > 1 << 22 || r->ld_hidden % unit || r->ld_head % unit) return VLA_E_SHAPE;
   if (((uintptr_t)r->hidden | (uintptr_t)r->head) & 15) return VLA_E_SHAPE;
   return VLA_OK;
 }
@@ -594,60 +753,126 @@ int check_call(const vla_head_rows* r, const Targets& t, bool grad, void* work, 
 }
 
 template <class T>
-RowTargets prepare(const Plan& w, const vla_head_rows& r, const Targets& t, const float* g, char* work, hipStream_t st) {
+HeadPack<T> head_pack(const Plan& w, const vla_head_rows& r, int n0, int N, bool transposed, char* work) {
+  return HeadPack<T>{(const T*)r.head + (size_t)n0 * r.ld_head, r.ld_head, min(N, w.V - n0), w.d, N, w.dP, (f16*)(work + w.wF),
+                     transposed ? (f16*)(work + w.wT) : nullptr};
+}
+
+// Rows and, if it is packed in one piece, the head.
+template <class T>
+RowTargets prepare(const Plan& w, const vla_head_rows& r, const Targets& t, const float* g, bool h_transposed, bool w_transposed,
+                   char* work, hipStream_t st) {
+  constexpr int TERMS = std::is_same_v<T, float> ? 3 : 1;
   auto f = [&](size_t o) { return (float*)(work + o); };
   const float tau = r.temperature > 0.f ? r.temperature : 1.0f;
-  const PrepOut out{f(w.z_scale), f(w.h_scale), g ? f(w.coef) : nullptr, g ? f(w.t_max) : nullptr, (int32_t*)(work + w.label),
-                    (int32_t*)(work + w.ids), f(w.p), f(w.ent), f(w.mass), (unsigned short*)(work + w.first)};
-  hipLaunchKernelGGL((loss_prep_kernel<T>), dim3(w.T), dim3(256), 0, st, (const T*)r.hidden, r.ld_hidden, w.d, w.V, 1.0f / tau,
-                     t.labels, t.top_logits, t.top_ids, w.k, w.groups, g, out);
+  const RowsOut out{f(w.z_scale), f(w.coef), f(w.dz_coef), f(w.dz_max), (int32_t*)(work + w.label), (int32_t*)(work + w.ids), f(w.p),
+                    f(w.ent), f(w.mass), (unsigned short*)(work + w.first), (f16*)(work + w.hF), h_transposed ? (f16*)(work + w.hT) : nullptr};
+  auto kern = loss_rows_kernel<T, TERMS>;
+  static bool attr_set = false;
+  if (!attr_set) {
+    (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * 12 * kMaxTop);
+    attr_set = true;
+  }
+  HeadPack<T> head{};
+  int wgs = w.Tp / 8;
+  if (!w.raw && w.pieces == 1) {
+    head = head_pack<T>(w, r, 0, w.Vp, w_transposed, work);
+    wgs += (w.dP / 64) * (w.Vp / 64) / 2;                            // (columns in pairs of tiles: dP and Vp are multiples of 128)
+  }
+  hipLaunchKernelGGL(kern, dim3(wgs), dim3(512), (size_t)96 * ((w.k + 3) & ~3), st, (const T*)r.hidden, r.ld_hidden, w.T, w.d, w.V,
+                     1.0f / tau, t.labels, t.top_logits, t.top_ids, w.k, w.groups, g, w.Tp, w.dP, out, head);
   return RowTargets{out.z_scale, w.k ? nullptr : out.label, out.ids, out.p, out.first, w.k, w.groups};
 }
 
-template <class T, bool B>
-void pack(const T* src, int64_t ld, int R, int C, int Rp, int Cp, float scale, const float* f_scale, const float* ft_row,
-          const float* ft_all, f16* F, f16* FT, hipStream_t st) {
+template <class T>
+void pack_piece(const Plan& w, const vla_head_rows& r, int n0, int N, bool transposed, char* work, hipStream_t st) {
   constexpr int TERMS = std::is_same_v<T, float> ? 3 : 1;
-  hipLaunchKernelGGL((loss_pack_kernel<T, TERMS, B>), dim3((Cp + 63) / 64, (Rp + 63) / 64), dim3(256), 0, st, src, ld, R, C, Rp,
-                     Cp, scale, f_scale, ft_row, ft_all, F, FT);
+  hipLaunchKernelGGL((loss_pack_kernel<T, TERMS>), dim3((w.dP / 64) * (N / 64)), dim3(256), 0, st,
+                     head_pack<T>(w, r, n0, N, transposed, work));
+}
+
+// Statistics of the whole vocabulary, and their sums.
+template <class T>
+void statistics(const Plan& w, const vla_head_rows& r, const RowTargets& tg, float* loss, float* lse, char* work, hipStream_t st) {
+  auto f = [&](size_t o) { return (float*)(work + o); };
+  const f16* hF = (const f16*)(work + w.hF);
+  const int ld = w.terms * w.dP;
+  bool done = false;
+  if constexpr (std::is_same_v<T, bf16>)
+    if (w.raw) {
+      product(hF, ld, r.head, w.T, w.Vp, w.d, EpiStats<1>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, 0, r.ld_head, w.V}, st);
+      done = true;
+    }
+  if (!done)
+    for (int n0 = 0; n0 < w.Vp; n0 += w.piece) {
+      const int N = min(w.piece, w.Vp - n0);
+      if (w.pieces > 1) pack_piece<T>(w, r, n0, N, false, work, st);
+      product(hF, ld, work + w.wF, w.T, N, ld, EpiStats<0>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, n0, 0, 0}, st);
+    }
+  hipLaunchKernelGGL(loss_join_kernel, dim3((w.T + 15) / 16), dim3(1024), 0, st, f(w.pm), f(w.pl), f(w.pa), w.T, w.groups, tg,
+                     f(w.ent), f(w.mass), loss, lse);
 }
 
 template <class T>
 int run_loss(const Plan& w, const vla_head_rows& r, const Targets& t, float* loss, float* lse, char* work, hipStream_t st) {
-  const RowTargets tg = prepare<T>(w, r, t, nullptr, work, st);
-  auto f = [&](size_t o) { return (float*)(work + o); };
-  f16 *hF = (f16*)(work + w.hF), *wF = (f16*)(work + w.wF);
-  pack<T, false>((const T*)r.hidden, r.ld_hidden, w.T, w.d, w.Tp, w.dP, 1.0f, f(w.h_scale), nullptr, nullptr, hF, nullptr, st);
-  pack<T, true>((const T*)r.head, r.ld_head, w.V, w.d, w.Vp, w.dP, kWeightScale, nullptr, nullptr, nullptr, wF, nullptr, st);
-  product(hF, wF, w.T, w.Vp, w.terms * w.dP, EpiStats{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, 0}, st);
-  hipLaunchKernelGGL(loss_join_kernel, dim3((w.T + 15) / 16), dim3(256), 0, st, f(w.pm), f(w.pl), f(w.pa), w.T, w.groups, tg,
-                     w.k ? f(w.ent) : nullptr, w.k ? f(w.mass) : nullptr, loss, lse);
+  const RowTargets tg = prepare<T>(w, r, t, nullptr, false, false, work, st);
+  statistics<T>(w, r, tg, loss, lse, work, st);
   return hipGetLastError() == hipSuccess ? VLA_OK : VLA_E_HIP;
 }
 
 template <class T>
 int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const float* lse, const float* g, void* gh, void* gw,
              char* work, hipStream_t st) {
-  const RowTargets tg = prepare<T>(w, r, t, g, work, st);
+  constexpr int TERMS = std::is_same_v<T, float> ? 3 : 1;
+  constexpr bool f32 = TERMS == 3;
+  const RowTargets tg = prepare<T>(w, r, t, g, gw != nullptr, gh != nullptr, work, st);
   auto f = [&](size_t o) { return (float*)(work + o); };
   auto h = [&](size_t o) { return (f16*)(work + o); };
-  const int out_f32 = std::is_same_v<T, float>;
-  hipLaunchKernelGGL(loss_scale_kernel, dim3(1), dim3(256), 0, st, f(w.t_max), w.T, f(w.scales));
-  pack<T, false>((const T*)r.hidden, r.ld_hidden, w.T, w.d, w.Tp, w.dP, 1.0f, f(w.h_scale), nullptr, nullptr, h(w.hF), nullptr, st);
-  if (gw) pack<T, true>((const T*)r.hidden, r.ld_hidden, w.T, w.d, w.Tp, w.dP, 1.0f, f(w.h_scale), f(w.coef), f(w.scales), nullptr, h(w.hT), st);
-  for (int n0 = 0; n0 < w.Vp; n0 += w.piece) {
-    const int N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
-    pack<T, true>((const T*)r.head + (size_t)n0 * r.ld_head, r.ld_head, rows, w.d, N, w.dP, kWeightScale, nullptr, nullptr, nullptr,
-                  h(w.wF), gh ? h(w.wT) : nullptr, st);
-    product(h(w.hF), h(w.wF), w.T, N, w.terms * w.dP,
-            EpiDz{tg, lse, gh ? h(w.dzF) : nullptr, gw ? h(w.dzT) : nullptr, w.Tp, N, w.terms, w.V, n0}, st);
-    if (gh)
-      product(h(w.dzF), h(w.wT), w.T, w.dP, w.terms * N,
-              EpiHidden{f(w.acc), w.dP, n0 == 0, n0 + N == w.Vp, f(w.coef), gh, out_f32, w.d}, st);
-    if (gw)
-      product(h(w.dzT), h(w.hT), N, w.dP, w.terms * w.Tp,
-              EpiHead{(T*)gw + (size_t)n0 * w.d, out_f32, w.d, rows, f(w.scales)}, st);
+  if (f32) {
+    statistics<T>(w, r, tg, nullptr, f(w.lse), work, st);
+    lse = f(w.lse);
   }
+  int n_max = w.Tp / 8;
+  if (n_max > 2048) {
+    hipLaunchKernelGGL(loss_max_kernel, dim3(1), dim3(256), 0, st, f(w.dz_max), n_max);
+    n_max = 1;
+  }
+  const int ld = TERMS * w.dP;
+  float* planes = w.planes ? f(w.planes) : nullptr;
+  for (int i = 0; i < w.pieces; ++i) {
+    const int n0 = i * w.piece, N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
+    float* set = planes ? planes + (size_t)(i % w.sets) * w.slices * w.T * w.dP : nullptr;
+    const int add = i >= w.sets;
+    const T* W = (const T*)r.head + (size_t)n0 * r.ld_head;
+    f16 *dzF = gh ? h(w.dzF) : nullptr, *dzT = gw ? h(w.dzT) : nullptr;
+    bool done = false;
+    if constexpr (!f32)
+      if (w.raw) {
+        product(h(w.hF), ld, W, w.T, N, w.d,
+                EpiDz<1, 1>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, r.ld_head, rows, 0.f}, st);
+        const int K = round_up(rows, PK);
+        if (gh)
+          product(dzF, N, W, w.T, w.dP, K,
+                  EpiHidden<2>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, 0, w.d,
+                               r.ld_head, rows, w.d}, st);
+        done = true;
+      }
+    if (!done) {
+      if (w.pieces > 1) pack_piece<T>(w, r, n0, N, gh != nullptr, work, st);
+      product(h(w.hF), ld, work + w.wF, w.T, N, ld,
+              EpiDz<0, TERMS>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, 0, 0, 0.f}, st);
+      if (gh)
+        product(dzF, TERMS * N, work + w.wT, w.T, w.dP, TERMS * N,
+                EpiHidden<0>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, f32, w.d,
+                             0, 0, 0}, st);
+    }
+    if (gw)
+      product(dzT, TERMS * w.Tp, h(w.hT), N, w.dP, TERMS * w.Tp,
+              EpiHead{(T*)gw + (size_t)n0 * w.d, f32, w.d, rows, f(w.dz_max), n_max, 0.f}, st);
+  }
+  if (gh && planes)
+    hipLaunchKernelGGL(loss_planes_kernel, dim3((w.d + 255) / 256, (w.T + 3) / 4), dim3(256), 0, st, planes, w.sets * w.slices, w.T, w.dP, w.d,
+                       f(w.coef), gh, (int)f32);
   return hipGetLastError() == hipSuccess ? VLA_OK : VLA_E_HIP;
 }
 

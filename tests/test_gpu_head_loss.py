@@ -99,6 +99,15 @@ def test_distill(T, d, V, k, dtype):
     check("distill", h, W, tgt, tau, coef, call("distill", h, W, tgt, tau, coef))
 
 
+@pytest.mark.parametrize("T,d,V", [(1, 512, 30000), (40, 768, 20001), (129, 512, 30000), (224, 512, 30001), (300, 768, 32003), (448, 1024, 31000),
+                                   (600, 4096, 24000), (700, 3968, 32000), (900, 320, 9000), (1300, 704, 4100), (2301, 128, 4003)])
+def test_sizes_of_every_tile(T, d, V):
+    """Heads that are read as they are and packed ones, rows that fill one to several tiles of each height."""
+    h, W, y, coef, _ = inputs(T, d, V, "bf16")
+    y[::7] = -1
+    check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
+
+
 def test_lists_of_the_largest_length_in_one_corner_of_the_vocabulary():
     T, d, V, k = 5, 128, 1500, 1024
     h, W, _, coef, g = inputs(T, d, V, "bf16")
