@@ -120,6 +120,7 @@ struct RowsOut {
 // Eight rows a workgroup, a wave each: the row's target and scale, then its h as operands.  The workgroups behind those of the
 // rows pack the head (two tiles each), where a call packs it in one piece: a launch less.
 constexpr int kRowsChunk = 1024;               // columns at a time
+constexpr int kRowsHeld = 4096;
 template <class T, int TERMS>
 __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h, int64_t ld, int Tn, int d, int V, float inv_tau,
                                                         const int32_t* __restrict__ labels, const float* __restrict__ top_logits,
@@ -232,14 +233,28 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
       out.first[(size_t)row * (groups + 1) + b] = (unsigned short)at;
     }
   }
+  // A row of up to kRowsHeld columns stays in registers between its maximum and its operands.
+  constexpr int N = Vec<T>::n, HELD = kRowsHeld / (64 * N);
+  typedef typename Vec<T>::type X;
   const T* x = h + (size_t)row * ld;
+  const bool held = d <= kRowsHeld;
+  X xv[HELD] = {};
   float mx = 0.f;
-  if (live)
-    for (int i = lane * Vec<T>::n; i < d; i += 64 * Vec<T>::n) {
-      const typename Vec<T>::type v = *(const typename Vec<T>::type*)(x + i);
+  auto max_of = [&](const X& v) {
 #pragma unroll
-      for (int j = 0; j < Vec<T>::n; ++j) mx = fmaxf(mx, fabsf((float)v[j]));
+    for (int j = 0; j < N; ++j) mx = fmaxf(mx, fabsf((float)v[j]));
+  };
+  if (live) {
+    if (held) {
+#pragma unroll
+      for (int u = 0; u < HELD; ++u)
+        if ((u * 64 + lane) * N < d) xv[u] = *(const X*)(x + (u * 64 + lane) * N);
+#pragma unroll
+      for (int u = 0; u < HELD; ++u) max_of(xv[u]);
+    } else {
+      for (int i = lane * N; i < d; i += 64 * N) max_of(*(const X*)(x + i));
     }
+  }
   mx = wave_max(mx);
   const int e = live ? scale_exponent(mx) : 0;
   const float scale = live ? ldexpf(1.0f, e) : 0.f;
@@ -260,16 +275,20 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
     for (int i = 1; i < 8; ++i) t = fmaxf(t, s_max[i]);
     out.dz_max[blockIdx.x] = t;
   }
-  for (int c0 = 0; c0 < dP; c0 += kRowsChunk) {
+  auto chunk = [&](int c0, auto U) __attribute__((always_inline)) {
+    constexpr int u0 = decltype(U)::value;                           // the chunk's first register, -1: read again
     const int n = min(kRowsChunk, dP - c0);
     if (c0) __syncthreads();
-    for (int i = lane * Vec<T>::n; i < n; i += 64 * Vec<T>::n) {
-      typename Vec<T>::type v;
-      const bool in = live && c0 + i < d;
-      if (in) v = *(const typename Vec<T>::type*)(x + c0 + i);
 #pragma unroll
-      for (int j = 0; j < Vec<T>::n; ++j) {
-        const float y = in ? (float)v[j] * scale : 0.f;
+    for (int u = 0; u < kRowsChunk / (64 * N); ++u) {
+      const int i = (u * 64 + lane) * N;
+      if (i >= n) break;
+      X v{};
+      if constexpr (u0 >= 0) v = xv[u0 + u];
+      else if (live && c0 + i < d) v = *(const X*)(x + c0 + i);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float y = live ? (float)v[j] * scale : 0.f;
         const f16 hi = from_f32<f16>(y);
         tile[0][wave * PITCH + i + j] = hi;
         if constexpr (TERMS == 3) tile[1][wave * PITCH + i + j] = from_f32<f16>(y - (float)hi);
@@ -300,7 +319,14 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
           *(f16x8*)(out.FT + act_index(c0 + i, 2 * Tp + row0, ldT)) = lo;
         }
       }
-  }
+  };
+  if (held)
+    static_for<kRowsHeld / kRowsChunk>([&](auto I) __attribute__((always_inline)) {
+      constexpr int c0 = decltype(I)::value * kRowsChunk;
+      if (c0 < dP) chunk(c0, std::integral_constant<int, c0 / (64 * N)>{});
+    });
+  else
+    for (int c0 = 0; c0 < dP; c0 += kRowsChunk) chunk(c0, std::integral_constant<int, -1>{});
 }
 
 // The largest of n values to the first of them (a launch of its own for what every wave of the products would have to read).
@@ -326,10 +352,6 @@ __device__ __forceinline__ int max_exponent(const float* v, int n, int lane) {
 
 // ---- operands in fragment order ---------------------------------------------------------------------------------
 // ---- epilogues -----------------------------------------------------------------------------------------------
-// z of an accumulated product.  An infinite weight makes an infinite product, which as -inf would count as a probability of 0:
-// anything infinite becomes a NaN.
-__device__ __forceinline__ float to_z(float x, float z_scale) { return fmaf(x, 0.f, x) * z_scale; }
-
 // Partial statistics of the groups of 64 columns.  ROWS rows of a group by 64 / ROWS lanes each; a group's sums are formed in
 // the same order whatever the tile, so a row's loss does not depend on the rows beside it.
 template <int RAW>
@@ -354,39 +376,42 @@ struct EpiStats {
       float x[W];
 #pragma unroll
       for (int i = 0; i < W; i += 4) *(f32x4*)(x + i) = *(const f32x4*)(tile + r * PITCH + c0 + i);
+      if (n0 + kGroup > V) {                             // (uniform) the last group
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] = i < left ? x[i] : -INFINITY;
+      }
       float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        x[i] = to_z(x[i], zs);
-        if (left < W) x[i] = i < left ? x[i] : -INFINITY;            // (uniform but for the lanes' parts)
-        mx = fmaxf(mx, x[i]);
-      }
-#pragma unroll
-      for (int s = ROWS; s < 64; s *= 2) mx = fmaxf(mx, __shfl_xor(mx, s, 64));
-      const float ref = mx == -INFINITY ? 0.f : mx;
-      float l = 0.f;                                     // sums of 16 columns, joined in pairs
+      for (int i = 0; i < W; ++i) mx = fmaxf(mx, x[i]);
+      mx = lanes_max<ROWS, 32>(mx);
+      const float z2 = zs * kLog2e, ref2 = mx == -INFINITY ? 0.f : -mx * z2;
+      // An infinite weight makes infinite products, which as -inf would count as probabilities of 0: `odd` is a NaN then.
+      float l = 0.f, odd = 0.f;                          // sums of 16 columns, joined in pairs
 #pragma unroll
       for (int h = 0; h < W / 16; ++h) {
         float s4[4] = {};
 #pragma unroll
-        for (int i = 16 * h; i < 16 * h + 16; ++i) s4[i & 3] += __builtin_amdgcn_exp2f((x[i] - ref) * kLog2e);
+        for (int i = 16 * h; i < 16 * h + 16; ++i) {
+          s4[i & 3] += __builtin_amdgcn_exp2f(fmaf(x[i], z2, ref2));
+          if (i < left) odd = fmaf(x[i], 0.f, odd);
+        }
         l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
       }
-#pragma unroll
-      for (int s = ROWS; s < 64; s *= 2) l += __shfl_xor(l, s, 64);
+      l += odd;
+      l = lanes_sum<ROWS, 32>(l);
       if (part == 0 && m < M && n0 < V) {
         if (tg.label) {
           const int c = label - n0;
-          if (c >= 0 && c < kGroup) pa[m] = to_z(tile[r * PITCH + gg * kGroup + c], zs);
+          if (c >= 0 && c < kGroup) pa[m] = tile[r * PITCH + gg * kGroup + c] * zs;
         } else {
           const unsigned short* f = tg.first + (size_t)m * (tg.groups + 1) + n0 / kGroup;
           for (int e = f[0], end = f[1]; e < end; ++e) {
             const size_t at = (size_t)m * tg.k + e;
-            pa[at] = tg.p[at] * to_z(tile[r * PITCH + gg * kGroup + tg.ids[at] - n0], zs);
+            pa[at] = tg.p[at] * (tile[r * PITCH + gg * kGroup + tg.ids[at] - n0] * zs);
           }
         }
         const size_t at = (size_t)(n0 / kGroup) * T + m;
-        pm[at] = mx;
+        pm[at] = mx == -INFINITY ? mx : mx * zs;
         pl[at] = l;
       }
     }
@@ -409,7 +434,6 @@ struct EpiDz {
   int raw_rows;
   float ft_scale;
   __device__ __forceinline__ void begin(int lane) { ft_scale = ldexpf(kDzScale, max_exponent(dz_max, n_max, lane)); }
-  template <bool B>
   __device__ __forceinline__ void put(f16* dst, int m, int k, int third, const float (&x)[8]) const {
     f16x8 hi;
 #pragma unroll
@@ -428,7 +452,9 @@ struct EpiDz {
     float* tile = const_cast<float*>(tile_in);
     constexpr int PARTS = 64 / ROWS, CH = COLS / 8;
     const int r = lane % ROWS, part = lane / ROWS, m = m_base + r, mc = min(m, M - 1);
-    const float zs = m < M ? tg.z_scale[mc] : 0.f, ls = lse[mc], ft = dz_coef[mc] * ft_scale;
+    // A row without target, and one past the last: zeros.  (A head that half precision does not hold has made lse a NaN.)
+    const float zs = m < M ? tg.z_scale[mc] : 0.f, z2 = zs * kLog2e, ref2 = zs != 0.f ? -lse[mc] * kLog2e : 0.f;
+    const float kd = zs != 0.f ? kDzScale : 0.f, ft = zs != 0.f ? dz_coef[mc] * ft_scale : 0.f;
     const int label = tg.label ? tg.label[mc] : -1;
 #pragma unroll
     for (int it = 0; it < CH / PARTS; ++it) {
@@ -436,11 +462,13 @@ struct EpiDz {
       float* x = tile + r * PITCH + c;
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float q = __builtin_amdgcn_exp2f((to_z(x[j], zs) - ls) * kLog2e);
-        v[j] = n + j == label ? q - 1.0f : q;
-      }
-      if (!tg.label && zs != 0.f && n < V) {
+      for (int j = 0; j < 8; ++j) v[j] = __builtin_amdgcn_exp2f(fmaf(x[j], z2, ref2));
+      if (tg.label) {
+        if ((unsigned)(label - n) < 8u) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] -= n + j == label ? 1.0f : 0.f;
+        }
+      } else if (zs != 0.f && n < V) {
         const unsigned short* f = tg.first + (size_t)m * (tg.groups + 1) + n / kGroup;
         for (int e = f[0], end = f[1]; e < end; ++e) {
           const int id = tg.ids[(size_t)m * tg.k + e];
@@ -449,16 +477,18 @@ struct EpiDz {
           for (int j = 0; j < 8; ++j) v[j] -= n + j == id ? p : 0.f;
         }
       }
+      if (n_base + nb + COLS > V || m_base + ROWS > M) {             // (uniform) columns and rows that are not there
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = zs != 0.f && n + j < V ? v[j] : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = n + j < V && m < M ? v[j] : 0.f;
+      }
       if (FT) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = zs != 0.f ? v[j] * ft : 0.f;
+        for (int j = 0; j < 8; ++j) x[j] = v[j] * ft;
       }
       if (F && m < Tp) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= kDzScale;
-        put<false>(F, m, nb + c, Np, v);
+        for (int j = 0; j < 8; ++j) v[j] *= kd;
+        put(F, m, nb + c, Np, v);
       }
     }
     if (FT) {
@@ -471,7 +501,7 @@ struct EpiDz {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = tile[(rc * 8 + j) * PITCH + c];
-        if (m_base + rc * 8 < Tp) put<false>(FT, nb + c, m_base + rc * 8, Tp, v);
+        if (m_base + rc * 8 < Tp) put(FT, nb + c, m_base + rc * 8, Tp, v);
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -479,14 +509,17 @@ struct EpiDz {
 };
 
 // Rounds four results to the storage type.
+template <bool ONCE = false>
 __device__ __forceinline__ void store_result(void* out, size_t at, bool f32, const f32x4& g) {
   if (f32) {
-    *(f32x4*)((float*)out + at) = g;
+    if constexpr (ONCE) __builtin_nontemporal_store(g, (f32x4*)((float*)out + at));
+    else *(f32x4*)((float*)out + at) = g;
   } else {
     bf16x4 o;
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = from_f32<bf16>(g[j]);
-    *(bf16x4*)((bf16*)out + at) = o;
+    if constexpr (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(u32x2, o), (u32x2*)((bf16*)out + at));
+    else *(bf16x4*)((bf16*)out + at) = o;
   }
 }
 
@@ -543,6 +576,58 @@ __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restric
   store_result(out, (size_t)m * d + c, out_f32, v * coef[m]);
 }
 
+// Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in their order and hands to the
+// epilogue, a wave 32 rows of 64 columns.
+template <int RAW>
+struct EpiPlanes {
+  static constexpr int kSpan = 64, kRaw = RAW;
+  static constexpr bool kSliced = true;
+  int slices;
+  float* planes;             // [slices][Tp][N]
+  int Tp, N;
+  int64_t raw_ld;
+  int raw_rows;
+  __device__ __forceinline__ void slice(int kz) { planes += (size_t)kz * Tp * N; }
+  template <int COLS, int PITCH, int ROWS>
+  __device__ __forceinline__ void consume(const float* tile, int m_base, int nb, int lane, int M) const {
+    constexpr int LPR = COLS / 4, RPI = 64 / LPR;
+    const int r0 = lane / LPR, c4 = (lane % LPR) * 4;
+#pragma unroll
+    for (int it = 0; it < ROWS / RPI; ++it) {
+      const int r = it * RPI + r0, m = m_base + r;
+      if (m < M) *(f32x4*)(planes + (size_t)m * N + nb + c4) = *(const f32x4*)(tile + r * PITCH + c4);
+    }
+  }
+};
+template <class Epi>
+__global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restrict__ planes, int slices, int Tp, int N, int M, Epi epi_in) {
+  constexpr int PITCH = 68;
+  __shared__ __attribute__((aligned(16))) float tiles[4][32 * PITCH];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int across = N / 64, id = blockIdx.x * 4 + wave, m0 = id / across * 32, n0 = id % across * 64;
+  if (m0 >= Tp) return;                                              // (whole waves; no barrier follows)
+  Epi epi = epi_in;
+  float* tile = tiles[wave];
+  const size_t plane = (size_t)Tp * N;
+  const float* p = planes + (size_t)(m0 + (lane >> 4)) * N + n0 + (lane & 15) * 4;
+  f32x4 v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = *(const f32x4*)(p + (size_t)(4 * i) * N);
+  for (int s = 1; s < slices; ++s) {
+    f32x4 u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = *(const f32x4*)(p + s * plane + (size_t)(4 * i) * N);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += u[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) *(f32x4*)(tile + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4) = v[i];
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+  if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
+  epi.template consume<64, PITCH, 32>(tile, m0, n0, lane, M);
+}
+
 // grad_head: rows of a piece of the vocabulary.
 struct EpiHead {
   static constexpr int kSpan = 64;
@@ -560,7 +645,7 @@ struct EpiHead {
     for (int it = 0; it < IT; ++it) {
       const int r = it * RPI + r0, m = m_base + r;
       const f32x4 g = *(const f32x4*)(tile + r * PITCH + c4) * scale;
-      if (m < rows && nb + c4 < d) store_result(out, (size_t)m * d + nb + c4, out_f32, g);
+      if (m < rows && nb + c4 < d) store_result<true>(out, (size_t)m * d + nb + c4, out_f32, g);
     }
   }
 };
@@ -575,7 +660,7 @@ static void product(const f16* A, int lda, const void* W, int M, int N, int K, c
   const GemmF16 g{A, lda, (const f16*)W, M, N, K, K, nullptr};
   constexpr bool four = std::is_same_v<Epi, EpiHidden<0>> || std::is_same_v<Epi, EpiHead>;    // 128x128 waves, as residual adds
   int n = N, k = K;
-  if constexpr (sliced<Epi>()) n = N * epi.slices, k = round_up(K / epi.slices, PK);          // (as in hidden_slices)
+  if constexpr (sliced<Epi>()) n = N * epi.slices, k = round_up(K / epi.slices, PK);          // (as in slices_of)
   int variant = gemm_f16_variant(M, n, k, k, false, Epi::kSpan);
   switch (variant) {
     case V_64x128_8W: launch<2, 4, 32, 32, 4, 4, 1, true, false, false>(g, epi, st); break;
@@ -651,17 +736,18 @@ struct Plan {
   int piece, pieces;           // columns of the vocabulary at a time (gradient)
   int slices;                  // of a piece, for grad_hidden, whose sums are in planes: of each slice, of up to four pieces
   int sets;                    // (later pieces add to the planes of earlier ones)
+  int z_slices;                // of the logits' products
   size_t z_scale, coef, dz_coef, dz_max, label, ids, p, ent, mass, first;
-  size_t hF, hT, wF, wT, dzF, dzT, planes, pm, pl, pa, lse, bytes;
+  size_t hF, hT, wF, wT, dzF, dzT, planes, zp, pm, pl, pa, lse, bytes;
 };
 
-// Slices of the contraction over K of grad_hidden: the number that the model of a launch's time, with the columns of all
-// slices beside one another, and the planes' bytes (written and read, 4 TB/s) make cheapest.
-int hidden_slices(int T, int dP, int K) {
+// Slices of the contraction of a product [T, N] over K: the number that the model of a launch's time, with the columns of all
+// slices beside one another, another launch and the planes' bytes (written and read, 4 TB/s) make cheapest.
+int slices_of(int T, int N, int K) {
   int best = 1;
-  float best_us = gemm_f16_model_us(T, dP, K);
+  float best_us = gemm_f16_model_us(T, N, K);
   for (int s = 2; s <= K / PK / 4 && s <= 64; s += s < 8 ? 1 : s < 16 ? 2 : 4) {
-    const float us = gemm_f16_model_us(T, dP * s, round_up(K / s, PK)) + 3.0f + (float)s * T * dP * 8e-6f / 4.0f;
+    const float us = gemm_f16_model_us(T, N * s, round_up(K / s, PK)) + 4.0f + (float)s * T * N * 8e-6f / 4.0f;
     if (us < best_us) best_us = us, best = s;
   }
   return best;
@@ -694,7 +780,7 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
     w.piece = w.pieces == 1 ? w.Vp : round_up((w.Vp + w.pieces - 1) / w.pieces, 256);
     w.pieces = (w.Vp + w.piece - 1) / w.piece;
     // (a slab at least in every slice of the last piece)
-    w.slices = min(hidden_slices(w.T, w.dP, w.terms * w.piece), (w.V - (w.pieces - 1) * w.piece + PK - 1) / PK);
+    w.slices = min(slices_of(w.T, w.dP, w.terms * w.piece), (w.V - (w.pieces - 1) * w.piece + PK - 1) / PK);
   }
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
@@ -706,6 +792,8 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   } else {
     w.label = take(4 * T);
   }
+  w.z_slices = w.pieces > 1 ? 1 : min(slices_of(w.T, w.Vp, w.terms * w.dP), (w.raw ? w.d : w.terms * w.dP) / PK);
+  if (w.z_slices > 1) w.zp = take(4 * (size_t)w.z_slices * w.Tp * w.Vp);
   w.hF = take((size_t)w.Tp * w.dP * half);
   if (!w.raw) w.wF = take((size_t)w.piece * w.dP * half);
   if (!grad || w.terms == 3) w.pm = take(4 * T * w.groups), w.pl = take(4 * T * w.groups), w.pa = take(4 * T * (k ? k : 1));
@@ -791,24 +879,38 @@ void pack_piece(const Plan& w, const vla_head_rows& r, int n0, int N, bool trans
                      head_pack<T>(w, r, n0, N, transposed, work));
 }
 
+// The logits of columns n0 .. n0 + N, of which `rows` are there, to the epilogue.
+template <class T, class Make>
+void logits(const Plan& w, const vla_head_rows& r, int n0, int N, int rows, char* work, Make&& make, hipStream_t st) {
+  const f16* hF = (const f16*)(work + w.hF);
+  const int ld = w.terms * w.dP;
+  const void* W = w.raw ? (const void*)((const T*)r.head + (size_t)n0 * r.ld_head) : (const void*)(work + w.wF);
+  float* zp = (float*)(work + w.zp);
+  auto run = [&](auto RAW, int K) {
+    constexpr int raw = decltype(RAW)::value;
+    const auto epi = make(RAW);
+    if (w.z_slices == 1) return product(hF, ld, W, w.T, N, K, epi, st);
+    product(hF, ld, W, w.T, N, K, EpiPlanes<raw>{w.z_slices, zp, w.Tp, N, r.ld_head, rows}, st);
+    hipLaunchKernelGGL((loss_slices_kernel<std::remove_const_t<decltype(epi)>>), dim3(((w.Tp / 32) * (N / 64) + 3) / 4), dim3(256), 0, st,
+                       zp, w.z_slices, w.Tp, N, w.T, epi);
+  };
+  if constexpr (std::is_same_v<T, bf16>) {
+    if (w.raw) return run(std::integral_constant<int, 1>{}, w.d);
+  }
+  run(std::integral_constant<int, 0>{}, ld);
+}
+
 // Statistics of the whole vocabulary, and their sums.
 template <class T>
 void statistics(const Plan& w, const vla_head_rows& r, const RowTargets& tg, float* loss, float* lse, char* work, hipStream_t st) {
   auto f = [&](size_t o) { return (float*)(work + o); };
-  const f16* hF = (const f16*)(work + w.hF);
-  const int ld = w.terms * w.dP;
-  bool done = false;
-  if constexpr (std::is_same_v<T, bf16>)
-    if (w.raw) {
-      product(hF, ld, r.head, w.T, w.Vp, w.d, EpiStats<1>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, 0, r.ld_head, w.V}, st);
-      done = true;
-    }
-  if (!done)
-    for (int n0 = 0; n0 < w.Vp; n0 += w.piece) {
-      const int N = min(w.piece, w.Vp - n0);
-      if (w.pieces > 1) pack_piece<T>(w, r, n0, N, false, work, st);
-      product(hF, ld, work + w.wF, w.T, N, ld, EpiStats<0>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, n0, 0, 0}, st);
-    }
+  for (int i = 0; i < w.pieces; ++i) {
+    const int n0 = i * w.piece, N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
+    if (!w.raw && w.pieces > 1) pack_piece<T>(w, r, n0, N, false, work, st);
+    logits<T>(w, r, n0, N, rows, work, [&](auto RAW) {
+      return EpiStats<decltype(RAW)::value>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, n0, r.ld_head, rows};
+    }, st);
+  }
   hipLaunchKernelGGL(loss_join_kernel, dim3((w.T + 15) / 16), dim3(1024), 0, st, f(w.pm), f(w.pl), f(w.pa), w.T, w.groups, tg,
                      f(w.ent), f(w.mass), loss, lse);
 }
@@ -837,35 +939,26 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
     hipLaunchKernelGGL(loss_max_kernel, dim3(1), dim3(256), 0, st, f(w.dz_max), n_max);
     n_max = 1;
   }
-  const int ld = TERMS * w.dP;
   float* planes = w.planes ? f(w.planes) : nullptr;
   for (int i = 0; i < w.pieces; ++i) {
     const int n0 = i * w.piece, N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
     float* set = planes ? planes + (size_t)(i % w.sets) * w.slices * w.T * w.dP : nullptr;
     const int add = i >= w.sets;
-    const T* W = (const T*)r.head + (size_t)n0 * r.ld_head;
     f16 *dzF = gh ? h(w.dzF) : nullptr, *dzT = gw ? h(w.dzT) : nullptr;
-    bool done = false;
+    if (!w.raw && w.pieces > 1) pack_piece<T>(w, r, n0, N, gh != nullptr, work, st);
+    logits<T>(w, r, n0, N, rows, work, [&](auto RAW) {
+      return EpiDz<decltype(RAW)::value, TERMS>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, r.ld_head, rows, 0.f};
+    }, st);
+    bool done = !gh;
     if constexpr (!f32)
-      if (w.raw) {
-        product(h(w.hF), ld, W, w.T, N, w.d,
-                EpiDz<1, 1>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, r.ld_head, rows, 0.f}, st);
-        const int K = round_up(rows, PK);
-        if (gh)
-          product(dzF, N, W, w.T, w.dP, K,
-                  EpiHidden<2>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, 0, w.d,
-                               r.ld_head, rows, w.d}, st);
+      if (w.raw && gh) {
+        product(dzF, N, (const T*)r.head + (size_t)n0 * r.ld_head, w.T, w.dP, round_up(rows, PK),
+                EpiHidden<2>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, 0, w.d, r.ld_head, rows, w.d}, st);
         done = true;
       }
-    if (!done) {
-      if (w.pieces > 1) pack_piece<T>(w, r, n0, N, gh != nullptr, work, st);
-      product(h(w.hF), ld, work + w.wF, w.T, N, ld,
-              EpiDz<0, TERMS>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, 0, 0, 0.f}, st);
-      if (gh)
-        product(dzF, TERMS * N, work + w.wT, w.T, w.dP, TERMS * N,
-                EpiHidden<0>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, f32, w.d,
-                             0, 0, 0}, st);
-    }
+    if (!done)
+      product(dzF, TERMS * N, work + w.wT, w.T, w.dP, TERMS * N,
+              EpiHidden<0>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, f32, w.d, 0, 0, 0}, st);
     if (gw)
       product(dzT, TERMS * w.Tp, h(w.hT), N, w.dP, TERMS * w.Tp,
               EpiHead{(T*)gw + (size_t)n0 * w.d, f32, w.d, rows, f(w.dz_max), n_max, 0.f}, st);
