@@ -448,9 +448,10 @@ struct TileCost { int bm, bn; float fixed, per_k, rate; };
 constexpr TileCost kTileCost[T_COUNT] = {{64, 128, 3.9f, 5.9f, 0.68f}, {128, 128, 4.3f, 7.4f, 0.92f},
                                          {64, 256, 6.8f, 9.3f, 0.80f}, {128, 256, 4.2f, 11.4f, 1.15f}, {192, 256, 8.0f, 13.7f, 1.25f},
                                          {256, 256, 10.9f, 16.1f, 1.30f}};
-struct TilePick { Tile tile; long long tiles; float us; };
+struct TilePick { Tile tile; long long tiles; };
 static TilePick pick_tile(int M, int N, int K) {
-  TilePick best{T_64x128, 0, 1e30f};
+  TilePick best{T_64x128, 0};
+  float best_us = 1e30f;
   for (int t = 0; t < T_COUNT; ++t) {
     const TileCost& c = kTileCost[t];
     if (N % c.bn) continue;
@@ -459,7 +460,10 @@ static TilePick pick_tile(int M, int N, int K) {
     const float per_tile = 2.0f * (float)c.bm * (float)c.bn * (float)K / (c.rate * 1e9f);      // us, full chip
     const long long rounds = tiles / 256, rest = tiles % 256;
     const float us = (float)rounds * fmaxf(alone, 256.0f * per_tile) + (rest ? fmaxf(alone, (float)rest * per_tile) : 0.f);
-    if (us < best.us) best = TilePick{(Tile)t, tiles, us};
+    if (us < best_us) {
+      best_us = us;
+      best = TilePick{(Tile)t, tiles};
+    }
   }
   return best;
 }
@@ -528,7 +532,6 @@ static FewTiles few_tiles(int M, int N, int K, int Kw) {
     }
   return {0, 0};
 }
-float gemm_f16_model_us(int M, int N, int K) { return pick_tile(M, N, K).us; }
 int gemm_f16_tile_rows(int M, int N, int K, int Kw, int span) {
   const int few = span == EpiResid::kSpan ? few_tiles(M, N, K, Kw).rows : 0;
   return few ? few : tile_rows(pick_tile(M, N, K), M, N);

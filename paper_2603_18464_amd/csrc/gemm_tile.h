@@ -180,6 +180,8 @@ constexpr int PK = 64;                                 // k of a slab (a slab of
 //   kRaw 2: W is bfloat16 rows [K, N], raw_ld apart, of which raw_rows (contraction) and raw_cols (a multiple of 8) exist;
 //        read transposed from the LDS.  raw_rows > K - 64; A must be zero where its contraction goes past raw_rows.
 //   kSliced: tiles of each of `slices` slices of the contraction; slice() is told which one.
+//   kPair: two products in one launch, the second one's operands, sizes and tiles in the epilogue, its workgroups from `split` (a
+//        multiple of 8) on; `second` tells the epilogue which it is.
 //   begin(lane): once a wave, in front of the first consume.
 template <class Epi> consteval int raw_w() {
   if constexpr (requires { Epi::kRaw; }) return Epi::kRaw;
@@ -188,6 +190,15 @@ template <class Epi> consteval int raw_w() {
 template <class Epi> consteval bool sliced() {
   if constexpr (requires { Epi::kSliced; }) return Epi::kSliced;
   else return false;
+}
+template <class Epi> consteval bool paired() {
+  if constexpr (requires { Epi::kPair; }) return Epi::kPair;
+  else return false;
+}
+template <class Epi> __device__ __forceinline__ int slices_of_launch(const Epi& e) {
+  if constexpr (paired<Epi>()) return e.second ? e.head.slices : e.hidden.slices;
+  else if constexpr (sliced<Epi>()) return e.slices;
+  else return 1;
 }
 template <class Epi> __device__ __forceinline__ int raw_rows_of(const Epi& e) {
   if constexpr (requires { e.raw_rows; }) return e.raw_rows;
@@ -294,13 +305,23 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
   // tiles, walked in groups of GM row-tiles that share the same weight columns (4 and 8 measure alike for the small
   // tiles and for those of 224 rows, 26 products within +-1.2 % and one 2.4 % better with 8; the 256-row tile is 4 % slower with 8
   // at 18560 rows, where the L2 then holds too few weight columns).
+  if constexpr (paired<Epi>()) {
+    if (blockIdx.x >= epi_in.split) {
+      A = epi_in.A, lda = epi_in.lda, Wp = epi_in.Wp, M = epi_in.M, K = Kw = epi_in.K, tiles_m = epi_in.tiles_m, tiles_n = epi_in.tiles_n;
+      epi_in.second = true;
+    }
+  }
   const int nblk = tiles_m * tiles_n;
-  const int per_xcd = gridDim.x >> 3;
+  int per_xcd = gridDim.x >> 3;
   int pid = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if constexpr (paired<Epi>()) {
+    per_xcd = (epi_in.second ? gridDim.x - epi_in.split : epi_in.split) >> 3;
+    pid = (blockIdx.x & 7) * per_xcd + ((epi_in.second ? blockIdx.x - epi_in.split : blockIdx.x) >> 3);
+  }
   int tm, tn, kz = 0;
   if constexpr (sliced<Epi>()) {
     kz = pid / nblk;
-    if (kz >= epi_in.slices) return;
+    if (kz >= slices_of_launch(epi_in)) return;
     pid -= kz * nblk;
   } else if (pid >= nblk) {
     return;
@@ -336,7 +357,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, OCC) void gemm_f16_kernel(const f16*
     epi.part += (size_t)kz * epi.plane_rows * epi.N;
   }
   if constexpr (sliced<Epi>()) {
-    const int u0 = (int)((long long)kz * KTw / epi.slices), u1 = (int)((long long)(kz + 1) * KTw / epi.slices);
+    const int u0 = (int)((long long)kz * KTw / slices_of_launch(epi)), u1 = (int)((long long)(kz + 1) * KTw / slices_of_launch(epi));
     kb0 = (size_t)u0 * KS16;
     KT = KTw = u1 - u0;
     epi.slice(kz);
@@ -642,7 +663,8 @@ template <int WGM, int WGN, int WM, int WN, int S, int SW, int OCC, bool DEEP, b
 static void launch_tiles(const f16* A, int lda, const f16* Wp, const f16* W8, int M, int K, int Kw, int tiles_m,
                          int tiles_n, const Epi& epi, hipStream_t st) {
   int wgs = tiles_m * tiles_n;
-  if constexpr (sliced<Epi>()) wgs *= epi.slices;
+  if constexpr (paired<Epi>()) wgs = (int)epi.split + epi.tiles_m * epi.tiles_n * epi.head.slices;
+  else if constexpr (sliced<Epi>()) wgs *= epi.slices;
   const int grid = (wgs + 7) / 8 * 8;
   constexpr size_t slabs = ((size_t)S * WGM * WM + (size_t)SW * WGN * WN) * PK * sizeof(f16);
   constexpr bool pair = WN < Epi::kSpan;

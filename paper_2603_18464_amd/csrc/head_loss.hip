@@ -34,6 +34,12 @@ struct RowTargets {
   const float* p;              // [T][k]
   const unsigned short* first; // [T][groups + 1] entry that begins each group of columns
   int k, groups;
+  // The entries of N - 1 groups of row m, from group g on, begin at at[0] .. (groups past the last have none).
+  template <int N>
+  __device__ __forceinline__ void entries(int m, int g, int (&at)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = first[(size_t)m * (groups + 1) + min(g + i, groups)];
+  }
 };
 
 template <class T> struct Vec;
@@ -46,6 +52,33 @@ __device__ __forceinline__ int scale_exponent(float x) {
   int e;
   (void)frexpf(x, &e);                     // x = f 2^e, f in [1/2, 1)
   return max(-60, min(60, 14 - e));
+}
+
+// The largest of n values to the first of them (a launch of its own for what every wave of the products would have to read).
+__global__ __launch_bounds__(256) void loss_max_kernel(float* __restrict__ v, int n) {
+  __shared__ float red[4];
+  float m = 0.f;
+  for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, v[i]);
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) v[0] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+// 2^x that brings the largest of n values into [1/2, 1); the same in every wave.
+__device__ __forceinline__ int max_exponent(const float* v, int n, int lane) {
+  float m = 0.f;
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, v[i]);
+  m = wave_max(m);
+  if (!(m > 0.f)) return 0;
+  int e;
+  (void)frexpf(m, &e);
+  return max(-120, min(120, -e));
+}
+
+// ---- operands in fragment order ---------------------------------------------------------------------------------
+// What brings the sums of grad_head back.
+__device__ __forceinline__ float head_scale(const float* dz_max, int n, int lane) {
+  return ldexpf(1.0f / kDzScale, -max_exponent(dz_max, n, lane));
 }
 
 // The head where it is not read as it is: 64 x 64 elements of src [R, C] by 256 threads, as rows (F [Rp, Cp], contraction over
@@ -142,12 +175,29 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   extern __shared__ __attribute__((aligned(16))) int32_t lists[];     // [8 rows][ids | keys | p], kp entries each
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = blockIdx.x * 8, row = row0 + wave;
+  int32_t target = -1;                         // the label, or the lane's first entry
+  float first_logit = 0.f;
+  if (row < Tn) {
+    if (labels) target = labels[row];
+    else if (lane < k) target = top_ids[(size_t)row * k + lane], first_logit = top_logits[(size_t)row * k + lane];
+  }
+  // A row of up to kRowsHeld columns is requested at once and stays in registers.
+  constexpr int N = Vec<T>::n, HELD = kRowsHeld / (64 * N);
+  typedef typename Vec<T>::type X;
+  const T* x = h + (size_t)row * ld;
+  const bool held = d <= kRowsHeld;
+  X xv[HELD] = {};
+  if (held && row < Tn) {
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+      if ((u * 64 + lane) * N < d) xv[u] = *(const X*)(x + (u * 64 + lane) * N);
+  }
+  const float g_row = g && row < Tn ? g[row] : 0.f;
   bool live = row < Tn;
   if (!live) {
   } else if (labels) {
-    const int32_t y = labels[row];
-    live = y >= 0 && y < V;
-    if (lane == 0) out.label[row] = live ? y : -1;
+    live = target >= 0 && target < V;
+    if (lane == 0) out.label[row] = live ? target : -1;
   } else {
     const int kp = (k + 3) & ~3;
     int32_t *s_id = lists + wave * 3 * kp, *s_key = s_id + kp;
@@ -157,8 +207,8 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
       int32_t id = -1;
       float l = 0.f;
       if (j < k) {
-        id = top_ids[(size_t)row * k + j];
-        l = top_logits[(size_t)row * k + j] * inv_tau;
+        id = j < 64 ? target : top_ids[(size_t)row * k + j];
+        l = (j < 64 ? first_logit : top_logits[(size_t)row * k + j]) * inv_tau;
         if (id < 0 || id >= V || l == -INFINITY) id = -1;
       }
       s_id[j] = id;
@@ -233,12 +283,6 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
       out.first[(size_t)row * (groups + 1) + b] = (unsigned short)at;
     }
   }
-  // A row of up to kRowsHeld columns stays in registers between its maximum and its operands.
-  constexpr int N = Vec<T>::n, HELD = kRowsHeld / (64 * N);
-  typedef typename Vec<T>::type X;
-  const T* x = h + (size_t)row * ld;
-  const bool held = d <= kRowsHeld;
-  X xv[HELD] = {};
   float mx = 0.f;
   auto max_of = [&](const X& v) {
 #pragma unroll
@@ -246,9 +290,6 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   };
   if (live) {
     if (held) {
-#pragma unroll
-      for (int u = 0; u < HELD; ++u)
-        if ((u * 64 + lane) * N < d) xv[u] = *(const X*)(x + (u * 64 + lane) * N);
 #pragma unroll
       for (int u = 0; u < HELD; ++u) max_of(xv[u]);
     } else {
@@ -262,7 +303,7 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   if (lane == 0 && row < Tn) {
     out.z_scale[row] = live ? ldexpf(inv_tau / kWeightScale, -e) : 0.f;
     if (g) {
-      const float c = live ? g[row] * inv_tau : 0.f, s = ldexpf(c, -e);
+      const float c = live ? g_row * inv_tau : 0.f, s = ldexpf(c, -e);
       out.coef[row] = c;
       out.dz_coef[row] = s;
       top = fabsf(s) < INFINITY ? fabsf(s) : 0.f;
@@ -329,28 +370,6 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
     for (int c0 = 0; c0 < dP; c0 += kRowsChunk) chunk(c0, std::integral_constant<int, -1>{});
 }
 
-// The largest of n values to the first of them (a launch of its own for what every wave of the products would have to read).
-__global__ __launch_bounds__(256) void loss_max_kernel(float* __restrict__ v, int n) {
-  __shared__ float red[4];
-  float m = 0.f;
-  for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, v[i]);
-  m = wave_max(m);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  if (threadIdx.x == 0) v[0] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
-// 2^x that brings the largest of n values into [1/2, 1); the same in every wave.
-__device__ __forceinline__ int max_exponent(const float* v, int n, int lane) {
-  float m = 0.f;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, v[i]);
-  m = wave_max(m);
-  if (!(m > 0.f)) return 0;
-  int e;
-  (void)frexpf(m, &e);
-  return max(-120, min(120, -e));
-}
-
-// ---- operands in fragment order ---------------------------------------------------------------------------------
 // ---- epilogues -----------------------------------------------------------------------------------------------
 // Partial statistics of the groups of 64 columns.  ROWS rows of a group by 64 / ROWS lanes each; a group's sums are formed in
 // the same order whatever the tile, so a row's loss does not depend on the rows beside it.
@@ -370,12 +389,18 @@ struct EpiStats {
     const int r = lane % ROWS, part = lane / ROWS, m = m_base + r, mc = min(m, M - 1);
     const float zs = tg.z_scale[mc];
     const int label = tg.label ? tg.label[mc] : -1;
+    int entry[COLS / kGroup + 1];                        // where the groups' entries begin
+    if (!tg.label) tg.entries(mc, (n_base + nb) / kGroup, entry);
 #pragma unroll
     for (int gg = 0; gg < COLS / kGroup; ++gg) {
       const int n0 = n_base + nb + gg * kGroup, c0 = gg * kGroup + part * W, left = V - n0 - part * W;
       float x[W];
 #pragma unroll
       for (int i = 0; i < W; i += 4) *(f32x4*)(x + i) = *(const f32x4*)(tile + r * PITCH + c0 + i);
+      // An infinite weight makes infinite products, which as -inf would count as probabilities of 0: `odd` is a NaN then.
+      float odd = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) odd = fmaf(x[i], 0.f, odd);
       if (n0 + kGroup > V) {                             // (uniform) the last group
 #pragma unroll
         for (int i = 0; i < W; ++i) x[i] = i < left ? x[i] : -INFINITY;
@@ -385,15 +410,13 @@ struct EpiStats {
       for (int i = 0; i < W; ++i) mx = fmaxf(mx, x[i]);
       mx = lanes_max<ROWS, 32>(mx);
       const float z2 = zs * kLog2e, ref2 = mx == -INFINITY ? 0.f : -mx * z2;
-      // An infinite weight makes infinite products, which as -inf would count as probabilities of 0: `odd` is a NaN then.
-      float l = 0.f, odd = 0.f;                          // sums of 16 columns, joined in pairs
+      float l = 0.f;                                     // sums of 16 columns, joined in pairs
 #pragma unroll
       for (int h = 0; h < W / 16; ++h) {
         float s4[4] = {};
 #pragma unroll
         for (int i = 16 * h; i < 16 * h + 16; ++i) {
           s4[i & 3] += __builtin_amdgcn_exp2f(fmaf(x[i], z2, ref2));
-          if (i < left) odd = fmaf(x[i], 0.f, odd);
         }
         l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
       }
@@ -404,8 +427,7 @@ struct EpiStats {
           const int c = label - n0;
           if (c >= 0 && c < kGroup) pa[m] = tile[r * PITCH + gg * kGroup + c] * zs;
         } else {
-          const unsigned short* f = tg.first + (size_t)m * (tg.groups + 1) + n0 / kGroup;
-          for (int e = f[0], end = f[1]; e < end; ++e) {
+          for (int e = entry[gg]; e < entry[gg + 1]; ++e) {
             const size_t at = (size_t)m * tg.k + e;
             pa[at] = tg.p[at] * (tile[r * PITCH + gg * kGroup + tg.ids[at] - n0] * zs);
           }
@@ -433,18 +455,19 @@ struct EpiDz {
   int64_t raw_ld;
   int raw_rows;
   float ft_scale;
-  __device__ __forceinline__ void begin(int lane) { ft_scale = ldexpf(kDzScale, max_exponent(dz_max, n_max, lane)); }
-  __device__ __forceinline__ void put(f16* dst, int m, int k, int third, const float (&x)[8]) const {
+  __device__ __forceinline__ void begin(int lane) { ft_scale = ldexpf(1.0f, max_exponent(dz_max, n_max, lane)); }
+  // 8 elements of an operand's row, and those of the second and third term (`third` halves on in a block of 32 rows).
+  __device__ __forceinline__ void put(f16* dst, size_t third, const float (&x)[8]) const {
     f16x8 hi;
 #pragma unroll
     for (int j = 0; j < 8; ++j) hi[j] = from_f32<f16>(x[j]);
-    *(f16x8*)(dst + act_index(m, k, TERMS * third)) = hi;
+    *(f16x8*)dst = hi;
     if constexpr (TERMS == 3) {
       f16x8 lo;
 #pragma unroll
       for (int j = 0; j < 8; ++j) lo[j] = from_f32<f16>(x[j] - (float)hi[j]);
-      *(f16x8*)(dst + act_index(m, third + k, 3 * third)) = lo;
-      *(f16x8*)(dst + act_index(m, 2 * third + k, 3 * third)) = hi;
+      *(f16x8*)(dst + third) = lo;
+      *(f16x8*)(dst + 2 * third) = hi;
     }
   }
   template <int COLS, int PITCH, int ROWS>
@@ -452,10 +475,30 @@ struct EpiDz {
     float* tile = const_cast<float*>(tile_in);
     constexpr int PARTS = 64 / ROWS, CH = COLS / 8;
     const int r = lane % ROWS, part = lane / ROWS, m = m_base + r, mc = min(m, M - 1);
-    // A row without target, and one past the last: zeros.  (A head that half precision does not hold has made lse a NaN.)
-    const float zs = m < M ? tg.z_scale[mc] : 0.f, z2 = zs * kLog2e, ref2 = zs != 0.f ? -lse[mc] * kLog2e : 0.f;
-    const float kd = zs != 0.f ? kDzScale : 0.f, ft = zs != 0.f ? dz_coef[mc] * ft_scale : 0.f;
+    // dz * 2^15; a row without target, and one past the last: zeros.  (A head that half precision does not hold has made lse a NaN.)
+    const bool live = m < M && tg.z_scale[mc] != 0.f;
+    const float z2 = live ? tg.z_scale[mc] * kLog2e : 0.f, ref2 = live ? fmaf(-lse[mc], kLog2e, 15.0f) : -INFINITY;
+    const float ft = live ? dz_coef[mc] * ft_scale : 0.f;
+    static_assert(kDzScale == 32768.0f, "2^15");
     const int label = tg.label ? tg.label[mc] : -1;
+    int entry[COLS / kGroup + 1] = {};                   // the row's entries here: entry[0] to entry[COLS / kGroup]
+    if (!tg.label) tg.entries(mc, (n_base + nb) / kGroup, entry);
+    const bool edge = n_base + nb + COLS > V || m_base + ROWS > M;   // (uniform) columns or rows that are not there
+    // Chunk `it` of a lane is 8 columns of its row; of the operand's blocks of 16 columns it is half `part` of block it, or (PARTS 4)
+    // half part & 1 of block 2 it + part / 2.
+    static_assert(PARTS == 2 || PARTS == 4, "as computed here");
+    f16* const f_at = F + (F ? act_index(m, nb, TERMS * Np) : 0) + (part >> 1) * 512 + (part & 1) * 256;
+    auto finish = [&](float* x, float (&v)[8], int it, int c) __attribute__((always_inline)) {
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = n_base + nb + c + j < V && m < M ? v[j] : 0.f;
+      }
+      if (FT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = v[j] * ft;
+      }
+      if (F && m < Tp) put(f_at + it * (PARTS / 2) * 512, (size_t)32 * Np, v);
+    };
 #pragma unroll
     for (int it = 0; it < CH / PARTS; ++it) {
       const int c = (it * PARTS + part) * 8, n = n_base + nb + c;
@@ -466,42 +509,50 @@ struct EpiDz {
       if (tg.label) {
         if ((unsigned)(label - n) < 8u) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] -= n + j == label ? 1.0f : 0.f;
+          for (int j = 0; j < 8; ++j) v[j] -= n + j == label ? kDzScale : 0.f;
         }
-      } else if (zs != 0.f && n < V) {
-        const unsigned short* f = tg.first + (size_t)m * (tg.groups + 1) + n / kGroup;
-        for (int e = f[0], end = f[1]; e < end; ++e) {
-          const int id = tg.ids[(size_t)m * tg.k + e];
-          const float p = tg.p[(size_t)m * tg.k + e];
+        finish(x, v, it, c);
+      } else {                                           // lists: the entries are taken off in the LDS
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] -= n + j == id ? p : 0.f;
+        for (int j = 0; j < 8; ++j) x[j] = v[j];
+      }
+    }
+    if (!tg.label) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_wave_barrier();
+      if (part == 0 && live)
+        for (int e = entry[0]; e < entry[COLS / kGroup]; ++e) {
+          const size_t at = (size_t)m * tg.k + e;
+          float* x = &tile[r * PITCH + tg.ids[at] - n_base - nb];
+          *x = fmaf(tg.p[at], -kDzScale, *x);
         }
-      }
-      if (n_base + nb + COLS > V || m_base + ROWS > M) {             // (uniform) columns and rows that are not there
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = n + j < V && m < M ? v[j] : 0.f;
-      }
-      if (FT) {
+      for (int it = 0; it < CH / PARTS; ++it) {
+        const int c = (it * PARTS + part) * 8;
+        float* x = tile + r * PITCH + c;
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = v[j] * ft;
-      }
-      if (F && m < Tp) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= kd;
-        put(F, m, nb + c, Np, v);
+        for (int j = 0; j < 8; ++j) v[j] = x[j];
+        finish(x, v, it, c);
       }
     }
     if (FT) {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
       __builtin_amdgcn_wave_barrier();
-      constexpr int RC = ROWS / 8;                       // chunks of 8 rows
+      // Eight rows (t) of a column (v) a lane: half lane / 32 of the blocks of 16 rows, of which there are RB, of 32 columns.
+      constexpr int RB = ROWS / 16;
+      const int rows0 = m_base + (lane >> 5) * 8;
+      f16* const t_at = FT + act_index(nb, m_base, TERMS * Tp) + lane * 8;
 #pragma unroll
-      for (int it = 0; it < COLS * RC / 64; ++it) {
-        const int i = (it * 64 + lane) >> 5, c = (i / RC) * 32 + (lane & 31), rc = i % RC;
+      for (int it = 0; it < COLS / 32 * RB; ++it) {
+        const int cb = it / RB, rb = it % RB;
+        const float* x = tile + (rb * 16 + (lane >> 5) * 8) * PITCH + cb * 32 + (lane & 31);
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = tile[(rc * 8 + j) * PITCH + c];
-        if (m_base + rc * 8 < Tp) put(FT, nb + c, m_base + rc * 8, Tp, v);
+        for (int j = 0; j < 8; ++j) v[j] = x[j * PITCH];
+        if (rows0 + rb * 16 < Tp) put(t_at + (size_t)cb * 32 * (TERMS * Tp) + rb * 512, (size_t)32 * Tp, v);
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -556,12 +607,15 @@ struct EpiHidden {
     }
   }
 };
-// ... and the planes in their order.
-__global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restrict__ planes, int n, int T, int ld, int d,
-                                                          const float* __restrict__ coef, void* __restrict__ out, int out_f32) {
-  const int c = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, m = blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (m >= T || c >= d) return;
-  const size_t plane = (size_t)T * ld;
+// ... and the planes in their order, times the rows' coefficients or (nullptr) what grad_head takes.
+__global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restrict__ planes, int n, int plane_rows, int ld, int rows,
+                                                          int d, const float* __restrict__ coef, const float* __restrict__ dz_max,
+                                                          int n_max, void* __restrict__ out, int out_f32) {
+  const int across = (d + 255) / 256, m = blockIdx.x / across * 4 + (threadIdx.x >> 6);
+  const int c = (blockIdx.x % across * 64 + (threadIdx.x & 63)) * 4;
+  const float scale = coef ? coef[min(m, rows - 1)] : head_scale(dz_max, n_max, threadIdx.x & 63);
+  if (m >= rows || c >= d) return;
+  const size_t plane = (size_t)plane_rows * ld;
   const float* p = planes + (size_t)m * ld + c;
   f32x4 v = *(const f32x4*)p;
   int i = 1;
@@ -573,7 +627,7 @@ __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restric
     for (int j = 0; j < 4; ++j) v += u[j];
   }
   for (; i < n; ++i) v += *(const f32x4*)(p + i * plane);
-  store_result(out, (size_t)m * d + c, out_f32, v * coef[m]);
+  store_result(out, (size_t)m * d + c, out_f32, v * scale);
 }
 
 // Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in their order and hands to the
@@ -613,30 +667,41 @@ __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restric
   f32x4 v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = *(const f32x4*)(p + (size_t)(4 * i) * N);
-  for (int s = 1; s < slices; ++s) {
-    f32x4 u[8];
+  if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
+  for (int s = 1; s < slices; s += 4) {                              // (a slice past the last: the last again, not added)
+    f32x4 u[4][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = *(const f32x4*)(p + s * plane + (size_t)(4 * i) * N);
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += u[i];
+      for (int i = 0; i < 8; ++i) u[j][i] = *(const f32x4*)(p + min(s + j, slices - 1) * plane + (size_t)(4 * i) * N);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (s + j < slices) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += u[j][i];
+      }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) *(f32x4*)(tile + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4) = v[i];
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __builtin_amdgcn_wave_barrier();
-  if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
   epi.template consume<64, PITCH, 32>(tile, m0, n0, lane, M);
 }
 
 // grad_head: rows of a piece of the vocabulary.
 struct EpiHead {
   static constexpr int kSpan = 64;
+  static constexpr bool kSliced = true;                // (of the rows)
+  int slices;
+  float* planes;             // [slices][M][ld], or nullptr
+  int plane, ld;             // rows of a plane
   void* out;                 // the piece's first row
   int out_f32, d, rows;
   const float* dz_max;
   int n_max;
   float scale;
-  __device__ __forceinline__ void begin(int lane) { scale = ldexpf(1.0f / kDzScale, -max_exponent(dz_max, n_max, lane)); }
+  __device__ __forceinline__ void begin(int lane) { scale = planes ? 1.0f : head_scale(dz_max, n_max, lane); }
+  __device__ __forceinline__ void slice(int kz) { if (planes) planes += (size_t)kz * plane * ld; }
   template <int COLS, int PITCH, int ROWS>
   __device__ __forceinline__ void consume(const float* tile, int m_base, int nb, int lane, int M) const {
     constexpr int LPR = COLS / 4, RPI = 64 / LPR, IT = ROWS / RPI;
@@ -645,34 +710,183 @@ struct EpiHead {
     for (int it = 0; it < IT; ++it) {
       const int r = it * RPI + r0, m = m_base + r;
       const f32x4 g = *(const f32x4*)(tile + r * PITCH + c4) * scale;
-      if (m < rows && nb + c4 < d) store_result<true>(out, (size_t)m * d + nb + c4, out_f32, g);
+      if (m >= rows || nb + c4 >= d) continue;
+      if (planes) *(f32x4*)(planes + (size_t)m * ld + nb + c4) = g;
+      else store_result<true>(out, (size_t)m * d + nb + c4, out_f32, g);
     }
+  }
+};
+
+// grad_head of at most 128 rows (bfloat16), where it is bound by what it writes: 64 rows of the head by 64 columns at a time a
+// wave, whose dz stays in registers while it walks 512 columns, straight from the accumulators.  The products are transposed (a row
+// of dz^T is a column here), and which columns of h a tile's rows are is chosen so that a lane holds eight in a row of each two
+// tiles, and the four groups of lanes 64 bytes.
+template <int KS>
+__global__ __launch_bounds__(256) void loss_head_rows_kernel(const f16* __restrict__ dzT, const f16* __restrict__ hT, int Tp,
+                                                             const float* __restrict__ dz_max, int n_max, bf16* __restrict__ out,
+                                                             int rows, int d) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, i = lane & 15, across = (d + 511) / 512, id = blockIdx.x * 4 + wave;
+  const int v0 = id / across * 64, c_first = id % across * 512;
+  if (v0 >= rows) return;                                            // (no barriers)
+  const size_t k_at = (size_t)(g >> 1) * 512 + (g & 1) * 256;        // of a k-step of 32: group g has k 8 g ..
+  f16x8 b[4][KS];
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      b[nt][ks] = *(const f16x8*)(dzT + (size_t)(v0 / 32 + nt / 2) * 32 * Tp + ks * 1024 + k_at + ((nt & 1) * 16 + i) * 8);
+  const float scale = head_scale(dz_max, n_max, lane);
+  auto load = [&](f16x8 (&a)[4][KS], int c0) {
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) {
+      const int c = c0 + 32 * (mt >> 1) + 8 * (i >> 2) + 4 * (mt & 1) + (i & 3);    // (columns past d: zeros of the operand, dP of them)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) a[mt][ks] = *(const f16x8*)(hT + (size_t)(c >> 5) * 32 * Tp + ks * 1024 + k_at + (c & 31) * 8);
+    }
+  };
+  const int c_end = min(c_first + 512, d);
+  f16x8 a[2][4][KS];
+  load(a[0], c_first);
+  auto columns = [&](f16x8 (&now)[4][KS], f16x8 (&next)[4][KS], int c0) __attribute__((always_inline)) {
+    if (c0 + 64 < c_end) load(next, c0 + 64);
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) {
+        acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now[mt][ks], b[nt][ks], acc[mt][nt], 0, 0, 0);
+      }
+    // Lanes of rows 8 apart swap a half, so that a store covers 128 bytes of 8 rows.
+    const bool up = i & 8;
+    const int c = c0 + 8 * g + (up ? 32 : 0);
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+      u32x4 o[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 e;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = from_f32<bf16>(acc[2 * h + (j >> 2)][nt][j & 3] * scale);
+        o[h] = __builtin_bit_cast(u32x4, e);
+      }
+      u32x4 s[2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned other = __builtin_bit_cast(unsigned, dpp<0x128>(__builtin_bit_cast(float, up ? o[0][j] : o[1][j])));   // row_ror 8
+        s[0][j] = up ? other : o[0][j];
+        s[1][j] = up ? o[1][j] : other;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int v = v0 + nt * 16 + h * 8 + (i & 7);
+        if (v < rows && c < d) {
+          __builtin_nontemporal_store(s[h], (u32x4*)(out + (size_t)v * d + c));
+        }
+      }
+    }
+  };
+  for (int c0 = c_first; c0 < c_end; c0 += 128) {
+    columns(a[0], a[1], c0);
+    if (c0 + 64 < c_end) columns(a[1], a[0], c0 + 64);
+  }
+}
+
+// Both gradients in one launch, where their tiles are the smallest ones: five microseconds less.
+struct EpiGradients {
+  static constexpr int kSpan = 64;
+  static constexpr bool kSliced = true, kPair = true;
+  EpiHidden<0> hidden;
+  EpiHead head;
+  unsigned split;
+  const f16 *A, *Wp;         // of the second, grad_head
+  int lda, M, K, tiles_m, tiles_n;
+  bool second;
+  __device__ __forceinline__ void begin(int lane) { if (second) head.begin(lane); }
+  __device__ __forceinline__ void slice(int kz) {
+    if (second) head.slice(kz);
+    else hidden.slice(kz);
+  }
+  template <int COLS, int PITCH, int ROWS>
+  __device__ __forceinline__ void consume(const float* tile, int m_base, int nb, int lane, int M) const {
+    if (second) head.consume<COLS, PITCH, ROWS>(tile, m_base, nb, lane, M);
+    else hidden.consume<COLS, PITCH, ROWS>(tile, m_base, nb, lane, M);
   }
 };
 
 static int round_up(int x, int n) { return (x + n - 1) / n * n; }
 static int tile_up(int x) { return x <= 128 ? 128 : round_up(x, 256); }        // columns of a product
 
-// The tiles of gemm_f16_variant, of which those of 64x256, 160x256 and 224x256 are run as their neighbours: EpiDz writes whole
-// blocks of 64 rows, and the difference does not pay for another instance each.
+// ---- tiles and slices -----------------------------------------------------------------------------------------------
+// Which tiles a product [M, N] over K takes, and into how many slices its contraction is split, goes by a model of its time: a
+// round of 256 workgroups (two rounds' worth of the 64x128 tiles that share a compute unit) takes `fixed`, by what the epilogue
+// does, and a time per 1024 k that grows from `few` on an empty chip to `full`.  Workgroups that fetch an operand from HBM take in
+// 65 GB/s each at best.  Fitted to 552 launches (32 to 32000 rows and columns, K 64 to 32000): us a launch, the model's pick and
+// others:
+//   statistics, 4096 x 32000 x 4096 753 (256x256; 192x256 801, 128x256 883, 128x128 1106), x 768 190 (202, 215, 256);
+//   1024 x 4096 x 4096 33 (128x128; 64x128 40, 256x256 73); 192 x 32000 x 4096 75 (128x256; 64x128 108); 64 x 4096 x 4096 18
+//   (64x128; 128x128 25, 256x256 68);
+//   grad_head 32000 x 4096 x 64 81 (192x256; 128x256 96, 128x128 128), x 4096 814 (256x256; 833, 903);
+//   grad_hidden 2048 x 4096 x 32000 in one slice 407 (128x256; 192x256 467, 256x256 557 of 128 tiles), in two of 256x256 365.
+// Unpacked weights cost 1.35 to 1.5 times the products (re-encoding) and have no 256x256 tile (registers).
+enum LossTile { L_64x128, L_64x128_PAIR, L_128x128, L_128x256, L_192x256, L_256x256, L_COUNT };
+enum LossWork { L_STATS, L_DZ, L_STORE };
+struct LossTileCost { int bm, bn, slots; float few, full, fixed[3]; };
+constexpr LossTileCost kLossTiles[L_COUNT] = {
+    {64, 128, 256, 3.5f, 5.8f, {0.7f, 5.0f, 2.6f}},    {64, 128, 512, 4.0f, 10.4f, {1.0f, 4.6f, 3.3f}},
+    {128, 128, 256, 5.0f, 8.0f, {2.0f, 8.3f, 3.5f}},   {128, 256, 256, 8.1f, 12.9f, {3.8f, 12.5f, 5.2f}},
+    {192, 256, 256, 11.5f, 17.0f, {6.0f, 15.0f, 6.3f}}, {256, 256, 256, 14.8f, 21.5f, {9.0f, 16.6f, 13.0f}}};
+struct LossPick { int tile, slices; float us; };
+static float launch_us(int t, LossWork work, int M, int N, int K, int slices, bool raw) {
+  const LossTileCost& c = kLossTiles[t];
+  const long long wgs = (long long)((M + c.bm - 1) / c.bm) * (N / c.bn) * slices;
+  const float k = (float)round_up(K / slices, PK) / 1024.0f;
+  float few = raw ? c.few * 1.35f : c.few, full = raw ? c.full * 1.5f : c.full;
+  if ((long long)K * (M > N ? M : N) > 64'000'000) few = fmaxf(few, (float)(c.bm + c.bn) * 2048.0f / 65e3f), full = fmaxf(full, few);
+  const float rounds = (float)(wgs / c.slots), rest = (float)(wgs % c.slots) / (float)c.slots;
+  return 2.0f + rounds * (c.fixed[work] + full * k) + (rest > 0.f ? c.fixed[work] + (few + (full - few) * rest) * k : 0.f);
+}
+// most: slices at most (1: not sliced).  Slices cost a launch that joins them and their planes, written and read at 4 TB/s.
+static LossPick pick_tiles(LossWork work, int M, int N, int K, int most, bool raw) {
+  LossPick best{L_64x128, 1, 1e30f};
+  for (int s = 1; s <= most; s += s < 8 ? 1 : s < 16 ? 2 : 4) {
+    const float join = s > 1 ? 5.0f + kLossTiles[0].fixed[work] + (float)s * (float)M * (float)N * 2e-6f : 0.f;
+    if (join > best.us) break;
+    for (int t = 0; t < (raw ? L_256x256 : L_COUNT); ++t) {
+      if (N % kLossTiles[t].bn) continue;
+      const float us = launch_us(t, s > 1 ? L_STORE : work, M, N, K, s, raw) + join;
+      if (us < best.us) best = LossPick{t, s, us};
+    }
+  }
+  return best;
+}
+
 template <class Epi>
-static void product(const f16* A, int lda, const void* W, int M, int N, int K, const Epi& epi, hipStream_t st) {
+static void product(int tile, const f16* A, int lda, const void* W, int M, int N, int K, const Epi& epi, hipStream_t st) {
   const GemmF16 g{A, lda, (const f16*)W, M, N, K, K, nullptr};
   constexpr bool four = std::is_same_v<Epi, EpiHidden<0>> || std::is_same_v<Epi, EpiHead>;    // 128x128 waves, as residual adds
-  int n = N, k = K;
-  if constexpr (sliced<Epi>()) n = N * epi.slices, k = round_up(K / epi.slices, PK);          // (as in slices_of)
-  int variant = gemm_f16_variant(M, n, k, k, false, Epi::kSpan);
-  switch (variant) {
-    case V_64x128_8W: launch<2, 4, 32, 32, 4, 4, 1, true, false, false>(g, epi, st); break;
-    case V_64x128: case V_64x128_ROUNDS: launch<2, 2, 32, 64, 3, 3, 2, false, false, false>(g, epi, st); break;
-    case V_128x128: launch<4, 2, 32, 64, 4, 4, 1, false, false, false>(g, epi, st); break;
-    case V_64x256: case V_128x256: launch<2, 4, 64, 64, 3, 3, 1, false, false, false>(g, epi, st); break;
-    case V_160x256: case V_192x256: launch<2, 4, 96, 64, 2, 3, 1, false, false, false>(g, epi, st); break;
+  switch (tile) {
+    case L_64x128: launch<2, 4, 32, 32, 4, 4, 1, true, false, false>(g, epi, st); break;
+    case L_64x128_PAIR: launch<2, 2, 32, 64, 3, 3, 2, false, false, false>(g, epi, st); break;
+    case L_128x128: launch<4, 2, 32, 64, 4, 4, 1, false, false, false>(g, epi, st); break;
+    case L_128x256: launch<2, 4, 64, 64, 3, 3, 1, false, false, false>(g, epi, st); break;
+    case L_192x256: launch<2, 4, 96, 64, 2, 3, 1, false, false, false>(g, epi, st); break;
     default:
-      if constexpr (raw_w<Epi>() != 0) launch<2, 4, 96, 64, 2, 3, 1, false, false, false>(g, epi, st);      // (registers)
+      if constexpr (raw_w<Epi>() != 0) launch<2, 4, 96, 64, 2, 3, 1, false, false, false>(g, epi, st);
       else if constexpr (four) launch<2, 2, 128, 128, 2, 3, 1, false, true, false>(g, epi, st);
       else launch<4, 2, 64, 128, 2, 3, 1, false, true, false>(g, epi, st);
   }
+}
+
+// Both gradients, dz [M, K] W [N, K] and the second's own product, in one launch of the smallest tiles.
+static void gradients(const f16* A, int lda, const f16* W, int M, int N, int K, const EpiHidden<0>& hidden, const f16* A2, int lda2,
+                      const f16* W2, int M2, int K2, const EpiHead& head, hipStream_t st) {
+  auto up = [](int x) { return (x + 63) / 64; };
+  const unsigned split = (unsigned)round_up(up(M) * (N / 128) * hidden.slices, 8);
+  const EpiGradients both{hidden, head, split, A2, W2, lda2, M2, K2, up(M2), N / 128, false};
+  launch<2, 4, 32, 32, 4, 4, 1, true, false, false>(GemmF16{A, lda, W, M, N, K, K, nullptr}, both, st);
 }
 
 // ---- joining the groups -------------------------------------------------------------------------------------------
@@ -720,9 +934,10 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(const float* __restrict
     }
   }
   if (part == 0 && row < T) {
-    const float n = (m == -INFINITY ? 0.f : m) + logf(l);
-    lse[row] = live ? n : 0.f;
-    if (loss) loss[row] = !live ? 0.f : tg.label ? n - pa[row] : ent[row] + mass[row] * n - a;
+    // (the difference to the largest logit first: it is exact, and nothing where that is the label's)
+    const float ref = m == -INFINITY ? 0.f : m, lg = logf(l);
+    lse[row] = live ? ref + lg : 0.f;
+    if (loss) loss[row] = !live ? 0.f : tg.label ? lg + (ref - pa[row]) : ent[row] + (mass[row] * lg + fmaf(mass[row], ref, -a));
   }
 }
 
@@ -734,35 +949,12 @@ struct Plan {
   int Tp, dP, Vp;              // padded sizes of operands: contractions in whole slabs, columns in whole tiles
   bool raw;                    // the head is read as it is
   int piece, pieces;           // columns of the vocabulary at a time (gradient)
-  int slices;                  // of a piece, for grad_hidden, whose sums are in planes: of each slice, of up to four pieces
-  int sets;                    // (later pieces add to the planes of earlier ones)
-  int z_slices;                // of the logits' products
+  LossPick z, stats;           // the logits' products (stats: of float32 with a gradient, which has both)
+  LossPick hidden, head;
+  int sets;                    // planes of grad_hidden: of each slice, of up to four pieces (later ones add to them)
   size_t z_scale, coef, dz_coef, dz_max, label, ids, p, ent, mass, first;
-  size_t hF, hT, wF, wT, dzF, dzT, planes, zp, pm, pl, pa, lse, bytes;
+  size_t hF, hT, wF, wT, dzF, dzT, planes, head_planes, zp, pm, pl, pa, lse, bytes;
 };
-
-// Slices of the contraction of a product [T, N] over K: the number that the model of a launch's time, with the columns of all
-// slices beside one another, another launch and the planes' bytes (written and read, 4 TB/s) make cheapest.
-int slices_of(int T, int N, int K) {
-  int best = 1;
-  float best_us = gemm_f16_model_us(T, N, K);
-  for (int s = 2; s <= K / PK / 4 && s <= 64; s += s < 8 ? 1 : s < 16 ? 2 : 4) {
-    const float us = gemm_f16_model_us(T, N * s, round_up(K / s, PK)) + 4.0f + (float)s * T * N * 8e-6f / 4.0f;
-    if (us < best_us) best_us = us, best = s;
-  }
-  return best;
-}
-
-// A bfloat16 head is read as it is where packing it (5 TB/s of twice its bytes, three times with a gradient) costs more than what
-// the products lose by re-encoding it between the LDS and the matrix cores (a third of their rate where they bound).  us, as it
-// is / packed, loss and gradient: 32000 x 4096 56 rows 57 / 148, 238 / 365, 384 rows 112 / 185, 425 / 525, 768 rows 202 / 258, 653 / 728,
-// 1536 rows 404 / 391, 1196 / 1148; 32000 x 768 56 rows 21 / 34, 54 / 73, 256 rows 31 / 39, 92 / 96, 512 rows 57 / 50, 160 / 133;
-// 8000 x 2048 256 rows 30 / 31, 70 / 71, 384 rows 45 / 35, 101 / 84; 2000 x 4096 one row 41 / 31, 56 / 52; 4000 x 1024 the same
-// within 5 % up to 384 rows.
-bool reads_head_as_it_is(int T, int d, int V) {
-  const long long size = (long long)d * V, least = 12'000'000;
-  return size >= least && T <= 256 + (size - least) / 256'000;
-}
 
 Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   Plan w{};
@@ -770,18 +962,37 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   w.terms = r.dtype == VLA_F32 ? 3 : 1;
   w.Tp = round_up(w.T, 64), w.dP = tile_up(w.d), w.Vp = tile_up(w.V);
   w.groups = (w.V + kGroup - 1) / kGroup;
-  w.raw = r.dtype == VLA_BF16 && w.d % PK == 0 && reads_head_as_it_is(w.T, w.d, w.V);
   const size_t half = 2 * (size_t)w.terms;
-  w.piece = w.Vp, w.pieces = w.slices = 1;
+  w.piece = w.Vp, w.pieces = 1;
   if (grad) {                                                       // dz, both ways, within 512 MB
     const size_t cols = (((size_t)512 << 20) / (2 * half * w.Tp)) & ~(size_t)255;
     const int most = cols < 256 ? 256 : cols > (size_t)w.Vp ? w.Vp : (int)cols;
     w.pieces = (w.Vp + most - 1) / most;
     w.piece = w.pieces == 1 ? w.Vp : round_up((w.Vp + w.pieces - 1) / w.pieces, 256);
     w.pieces = (w.Vp + w.piece - 1) / w.piece;
-    // (a slab at least in every slice of the last piece)
-    w.slices = min(slices_of(w.T, w.dP, w.terms * w.piece), (w.V - (w.pieces - 1) * w.piece + PK - 1) / PK);
   }
+  // Slices: a slab at least in each (of four, but for the last piece's).
+  const int Kz = w.terms * w.dP, Kh = w.terms * w.piece, Kw = w.terms * w.Tp;
+  const int last = (w.V - (w.pieces - 1) * w.piece + PK - 1) / PK;
+  auto most = [](int K) { return max(1, min(64, K / PK / 4)); };
+  auto picks = [&](bool raw) {
+    const int z_most = w.pieces > 1 ? 1 : raw ? most(w.d) : most(Kz);
+    w.z = pick_tiles(grad ? L_DZ : L_STATS, w.T, w.piece, raw ? w.d : Kz, z_most, raw);
+    w.stats = w.terms == 3 && grad ? w.z.slices > 1 ? w.z : pick_tiles(L_STATS, w.T, w.piece, Kz, 1, false) : w.z;
+    if (grad) w.hidden = pick_tiles(L_STORE, w.T, w.dP, Kh, min(most(Kh), last), raw);
+    return (w.z.us + (grad ? w.hidden.us : 0.f)) * (float)w.pieces;
+  };
+  const float packed = picks(false);
+  // A bfloat16 head is read as it is where packing it (5 TB/s of twice its bytes, three times with a gradient) costs more.  us, as
+  // it is / packed, loss and gradient: 32000 x 4096 56 rows 57 / 148, 238 / 365, 384 rows 112 / 185, 425 / 525, 768 rows 202 / 258,
+  // 653 / 728, 1536 rows 404 / 391, 1196 / 1148; 32000 x 768 56 rows 21 / 34, 54 / 73, 256 rows 31 / 39, 92 / 96, 512 rows 57 / 50,
+  // 160 / 133; 8000 x 2048 256 rows 30 / 31, 70 / 71, 384 rows 45 / 35, 101 / 84; 4000 x 1024 the same within 5 % up to 384 rows.
+  if (r.dtype == VLA_BF16 && w.d % PK == 0) {
+    const float raw = picks(true);
+    w.raw = raw < packed + (float)w.V * (float)w.d * (grad ? 6e-6f : 4e-6f) / 5.0f;
+    if (!w.raw) picks(false);
+  }
+  if (grad) w.head = pick_tiles(L_STORE, w.Vp, w.dP, Kw, w.pieces > 1 ? 1 : most(Kw), false);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
   const size_t T = (size_t)w.T;
@@ -792,8 +1003,7 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   } else {
     w.label = take(4 * T);
   }
-  w.z_slices = w.pieces > 1 ? 1 : min(slices_of(w.T, w.Vp, w.terms * w.dP), (w.raw ? w.d : w.terms * w.dP) / PK);
-  if (w.z_slices > 1) w.zp = take(4 * (size_t)w.z_slices * w.Tp * w.Vp);
+  if (w.z.slices > 1) w.zp = take(4 * (size_t)w.z.slices * w.Tp * w.Vp);
   w.hF = take((size_t)w.Tp * w.dP * half);
   if (!w.raw) w.wF = take((size_t)w.piece * w.dP * half);
   if (!grad || w.terms == 3) w.pm = take(4 * T * w.groups), w.pl = take(4 * T * w.groups), w.pa = take(4 * T * (k ? k : 1));
@@ -803,11 +1013,24 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
     if (!w.raw) w.wT = take((size_t)w.piece * w.dP * half);
     w.dzF = take((size_t)w.Tp * w.piece * half), w.dzT = take((size_t)w.Tp * w.piece * half);
     w.sets = min(w.pieces, 4);
-    if (w.sets * w.slices > 1) w.planes = take(4 * T * w.dP * w.sets * w.slices);
+    if (w.sets * w.hidden.slices > 1) w.planes = take(4 * T * w.dP * w.sets * w.hidden.slices);
+    if (w.head.slices > 1) w.head_planes = take(4 * (size_t)w.head.slices * w.Vp * w.dP);
     if (w.terms == 3) w.lse = take(4 * T);
   }
   w.bytes = at;
   return w;
+}
+
+// The last plans of this thread (some microseconds each), by the sizes that they depend on.
+const Plan& plan_of(const vla_head_rows& r, int k, bool grad) {
+  struct Kept { int T, d, V, dtype, k, grad; Plan plan; };
+  static thread_local Kept kept[16] = {};
+  static thread_local unsigned next = 0;
+  for (const Kept& e : kept)
+    if (e.T == r.n_rows && e.d == r.d_model && e.V == r.vocab && e.dtype == r.dtype && e.k == k && e.grad == (int)grad) return e.plan;
+  Kept& e = kept[next++ % 16];
+  e = Kept{r.n_rows, r.d_model, r.vocab, r.dtype, k, (int)grad, make_plan(r, k, grad)};
+  return e.plan;
 }
 
 int check_rows(const vla_head_rows* r, bool pointers) {
@@ -836,7 +1059,7 @@ int check_call(const vla_head_rows* r, const Targets& t, bool grad, void* work, 
   if (rc) return rc;
   if (!work || (t.k ? !t.top_logits || !t.top_ids : !t.labels)) return VLA_E_NULL;
   if ((uintptr_t)work & 255) return VLA_E_SHAPE;
-  *plan = make_plan(*r, t.k, grad);
+  *plan = plan_of(*r, t.k, grad);
   return work_bytes < plan->bytes ? VLA_E_CAPACITY : VLA_OK;
 }
 
@@ -881,7 +1104,7 @@ void pack_piece(const Plan& w, const vla_head_rows& r, int n0, int N, bool trans
 
 // The logits of columns n0 .. n0 + N, of which `rows` are there, to the epilogue.
 template <class T, class Make>
-void logits(const Plan& w, const vla_head_rows& r, int n0, int N, int rows, char* work, Make&& make, hipStream_t st) {
+void logits(const Plan& w, const LossPick& pick, const vla_head_rows& r, int n0, int N, int rows, bool have_planes, char* work, Make&& make, hipStream_t st) {
   const f16* hF = (const f16*)(work + w.hF);
   const int ld = w.terms * w.dP;
   const void* W = w.raw ? (const void*)((const T*)r.head + (size_t)n0 * r.ld_head) : (const void*)(work + w.wF);
@@ -889,10 +1112,10 @@ void logits(const Plan& w, const vla_head_rows& r, int n0, int N, int rows, char
   auto run = [&](auto RAW, int K) {
     constexpr int raw = decltype(RAW)::value;
     const auto epi = make(RAW);
-    if (w.z_slices == 1) return product(hF, ld, W, w.T, N, K, epi, st);
-    product(hF, ld, W, w.T, N, K, EpiPlanes<raw>{w.z_slices, zp, w.Tp, N, r.ld_head, rows}, st);
+    if (pick.slices == 1) return product(pick.tile, hF, ld, W, w.T, N, K, epi, st);
+    if (!have_planes) product(pick.tile, hF, ld, W, w.T, N, K, EpiPlanes<raw>{pick.slices, zp, w.Tp, N, r.ld_head, rows}, st);
     hipLaunchKernelGGL((loss_slices_kernel<std::remove_const_t<decltype(epi)>>), dim3(((w.Tp / 32) * (N / 64) + 3) / 4), dim3(256), 0, st,
-                       zp, w.z_slices, w.Tp, N, w.T, epi);
+                       zp, pick.slices, w.Tp, N, w.T, epi);
   };
   if constexpr (std::is_same_v<T, bf16>) {
     if (w.raw) return run(std::integral_constant<int, 1>{}, w.d);
@@ -907,7 +1130,7 @@ void statistics(const Plan& w, const vla_head_rows& r, const RowTargets& tg, flo
   for (int i = 0; i < w.pieces; ++i) {
     const int n0 = i * w.piece, N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
     if (!w.raw && w.pieces > 1) pack_piece<T>(w, r, n0, N, false, work, st);
-    logits<T>(w, r, n0, N, rows, work, [&](auto RAW) {
+    logits<T>(w, w.stats, r, n0, N, rows, false, work, [&](auto RAW) {
       return EpiStats<decltype(RAW)::value>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, n0, r.ld_head, rows};
     }, st);
   }
@@ -934,6 +1157,7 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
     statistics<T>(w, r, tg, nullptr, f(w.lse), work, st);
     lse = f(w.lse);
   }
+  const bool have_planes = f32 && w.z.slices > 1;                    // (of the logits, from their statistics)
   int n_max = w.Tp / 8;
   if (n_max > 2048) {
     hipLaunchKernelGGL(loss_max_kernel, dim3(1), dim3(256), 0, st, f(w.dz_max), n_max);
@@ -942,30 +1166,40 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
   float* planes = w.planes ? f(w.planes) : nullptr;
   for (int i = 0; i < w.pieces; ++i) {
     const int n0 = i * w.piece, N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
-    float* set = planes ? planes + (size_t)(i % w.sets) * w.slices * w.T * w.dP : nullptr;
+    float* set = planes ? planes + (size_t)(i % w.sets) * w.hidden.slices * w.T * w.dP : nullptr;
     const int add = i >= w.sets;
     f16 *dzF = gh ? h(w.dzF) : nullptr, *dzT = gw ? h(w.dzT) : nullptr;
     if (!w.raw && w.pieces > 1) pack_piece<T>(w, r, n0, N, gh != nullptr, work, st);
-    logits<T>(w, r, n0, N, rows, work, [&](auto RAW) {
+    logits<T>(w, w.z, r, n0, N, rows, have_planes, work, [&](auto RAW) {
       return EpiDz<decltype(RAW)::value, TERMS>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, r.ld_head, rows, 0.f};
     }, st);
-    bool done = !gh;
+    const EpiHead head{w.head.slices, w.head_planes ? f(w.head_planes) : nullptr, w.Vp, w.dP, (T*)gw + (size_t)n0 * w.d, f32, w.d, rows,
+                       f(w.dz_max), n_max, 0.f};
+    const EpiHidden<0> hidden{w.hidden.slices, set, add, w.T, w.dP, f(w.coef), gh, f32, w.d, 0, 0, 0};
+    const int K = TERMS * N, K2 = TERMS * w.Tp;
+    if (!w.raw && gh && gw && w.hidden.tile == L_64x128 && w.head.tile == L_64x128) {
+      gradients(dzF, K, h(w.wT), w.T, w.dP, K, hidden, dzT, K2, h(w.hT), N, K2, head, st);
+      continue;
+    }
     if constexpr (!f32)
-      if (w.raw && gh) {
-        product(dzF, N, (const T*)r.head + (size_t)n0 * r.ld_head, w.T, w.dP, round_up(rows, PK),
-                EpiHidden<2>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, 0, w.d, r.ld_head, rows, w.d}, st);
-        done = true;
-      }
-    if (!done)
-      product(dzF, TERMS * N, work + w.wT, w.T, w.dP, TERMS * N,
-              EpiHidden<0>{w.slices, set, add, w.T, w.dP, f(w.coef), gh, f32, w.d, 0, 0, 0}, st);
-    if (gw)
-      product(dzT, TERMS * w.Tp, h(w.hT), N, w.dP, TERMS * w.Tp,
-              EpiHead{(T*)gw + (size_t)n0 * w.d, f32, w.d, rows, f(w.dz_max), n_max, 0.f}, st);
+      if (w.raw && gh)
+        product(w.hidden.tile, dzF, N, (const T*)r.head + (size_t)n0 * r.ld_head, w.T, w.dP, round_up(rows, PK),
+                EpiHidden<2>{w.hidden.slices, set, add, w.T, w.dP, f(w.coef), gh, 0, w.d, r.ld_head, rows, w.d}, st);
+    if (!w.raw && gh) product(w.hidden.tile, dzF, K, work + w.wT, w.T, w.dP, K, hidden, st);
+    if (gw && !f32 && w.Tp <= 128) {
+      const dim3 grid((unsigned)(((rows + 63) / 64) * ((w.d + 511) / 512) + 3) / 4);
+      auto kern = w.Tp == 64 ? loss_head_rows_kernel<2> : loss_head_rows_kernel<4>;
+      hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, dzT, h(w.hT), w.Tp, f(w.dz_max), n_max, (bf16*)gw + (size_t)n0 * w.d, rows, w.d);
+      continue;
+    }
+    if (gw) product(w.head.tile, dzT, K2, h(w.hT), N, w.dP, K2, head, st);
   }
-  if (gh && planes)
-    hipLaunchKernelGGL(loss_planes_kernel, dim3((w.d + 255) / 256, (w.T + 3) / 4), dim3(256), 0, st, planes, w.sets * w.slices, w.T, w.dP, w.d,
-                       f(w.coef), gh, (int)f32);
+  auto join = [&](const float* from, int n, int plane_rows, int rows, const float* coef, void* out) {
+    hipLaunchKernelGGL(loss_planes_kernel, dim3((w.d + 255) / 256 * ((rows + 3) / 4)), dim3(256), 0, st, from, n, plane_rows, w.dP, rows,
+                       w.d, coef, f(w.dz_max), n_max, out, (int)f32);
+  };
+  if (gh && planes) join(planes, w.sets * w.hidden.slices, w.T, w.T, f(w.coef), gh);
+  if (gw && w.head_planes) join(f(w.head_planes), w.head.slices, w.Vp, w.V, nullptr, gw);
   return hipGetLastError() == hipSuccess ? VLA_OK : VLA_E_HIP;
 }
 

@@ -100,7 +100,8 @@ def test_distill(T, d, V, k, dtype):
 
 
 @pytest.mark.parametrize("T,d,V", [(1, 512, 30000), (40, 768, 20001), (129, 512, 30000), (224, 512, 30001), (300, 768, 32003), (448, 1024, 31000),
-                                   (600, 4096, 24000), (700, 3968, 32000), (900, 320, 9000), (1300, 704, 4100), (2301, 128, 4003)])
+                                   (600, 4096, 24000), (700, 3968, 32000), (900, 320, 9000), (1300, 704, 4100), (2301, 128, 4003), (100, 1024, 20000), (128, 520, 21000),
+                                   (65, 2048, 9000), (7954, 384, 256), (3000, 128, 200), (5000, 1536, 320)])
 def test_sizes_of_every_tile(T, d, V):
     """Heads that are read as they are and packed ones, rows that fill one to several tiles of each height."""
     h, W, y, coef, _ = inputs(T, d, V, "bf16")
