@@ -150,7 +150,8 @@ struct RowsOut {
   f16 *F, *FT;                                 // h in fragment order: rows [Tp, dP], and transposed [dP, Tp] (or nullptr)
 };
 
-// Eight rows a workgroup, a wave each: the row's target and scale, then its h as operands.  The workgroups behind those of the
+// Eight rows a workgroup, a wave each: the row's target and scale, then its h as operands; of few rows `splits` workgroups, which
+// take the chunks of columns in turn (each finds the scale for itself).  The workgroups behind those of the
 // rows pack the head (two tiles each), where a call packs it in one piece: a launch less.
 constexpr int kRowsChunk = 1024;               // columns at a time
 constexpr int kRowsHeld = 4096;
@@ -158,7 +159,7 @@ template <class T, int TERMS>
 __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h, int64_t ld, int Tn, int d, int V, float inv_tau,
                                                         const int32_t* __restrict__ labels, const float* __restrict__ top_logits,
                                                         const int32_t* __restrict__ top_ids, int k, int groups,
-                                                        const float* __restrict__ g, int Tp, int dP, RowsOut out,
+                                                        const float* __restrict__ g, int Tp, int dP, int splits, RowsOut out,
                                                         HeadPack<T> head) {
   constexpr int PITCH = kRowsChunk + 8;
   __shared__ union {
@@ -166,15 +167,16 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
     float head[2][64][65];
   } s_tile;
   __shared__ float s_max[8];
-  if ((int)blockIdx.x >= Tp / 8) {
+  if ((int)blockIdx.x >= Tp / 8 * splits) {
     const int half = threadIdx.x >> 8;
-    pack_tile<T, TERMS>(head, ((int)blockIdx.x - Tp / 8) * 2 + half, threadIdx.x & 255, s_tile.head[half]);
+    pack_tile<T, TERMS>(head, ((int)blockIdx.x - Tp / 8 * splits) * 2 + half, threadIdx.x & 255, s_tile.head[half]);
     return;
   }
   auto& tile = s_tile.row;
   extern __shared__ __attribute__((aligned(16))) int32_t lists[];     // [8 rows][ids | keys | p], kp entries each
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = blockIdx.x * 8, row = row0 + wave;
+  const int row0 = (int)blockIdx.x / splits * 8, row = row0 + wave, split = (int)blockIdx.x % splits;
+  const bool first = split == 0;               // (what there is one of for a row)
   int32_t target = -1;                         // the label, or the lane's first entry
   float first_logit = 0.f;
   if (row < Tn) {
@@ -197,7 +199,14 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   if (!live) {
   } else if (labels) {
     live = target >= 0 && target < V;
-    if (lane == 0) out.label[row] = live ? target : -1;
+    if (lane == 0 && first) out.label[row] = live ? target : -1;
+  } else if (!first) {
+    bool any = target >= 0 && target < V && first_logit * inv_tau != -INFINITY;
+    for (int j = lane + 64; j < k; j += 64) {
+      const int32_t id = top_ids[(size_t)row * k + j];
+      any = any || (id >= 0 && id < V && top_logits[(size_t)row * k + j] * inv_tau != -INFINITY);
+    }
+    live = __any(any);
   } else {
     const int kp = (k + 3) & ~3;
     int32_t *s_id = lists + wave * 3 * kp, *s_key = s_id + kp;
@@ -300,7 +309,7 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   const int e = live ? scale_exponent(mx) : 0;
   const float scale = live ? ldexpf(1.0f, e) : 0.f;
   float top = 0.f;
-  if (lane == 0 && row < Tn) {
+  if (lane == 0 && row < Tn && first) {
     out.z_scale[row] = live ? ldexpf(inv_tau / kWeightScale, -e) : 0.f;
     if (g) {
       const float c = live ? g_row * inv_tau : 0.f, s = ldexpf(c, -e);
@@ -311,15 +320,17 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   }
   if (lane == 0) s_max[wave] = top;
   __syncthreads();
-  if (g && threadIdx.x == 0) {
+  if (g && threadIdx.x == 0 && first) {
     float t = s_max[0];
     for (int i = 1; i < 8; ++i) t = fmaxf(t, s_max[i]);
-    out.dz_max[blockIdx.x] = t;
+    out.dz_max[row0 / 8] = t;
   }
+  bool again = false;
   auto chunk = [&](int c0, auto U) __attribute__((always_inline)) {
     constexpr int u0 = decltype(U)::value;                           // the chunk's first register, -1: read again
     const int n = min(kRowsChunk, dP - c0);
-    if (c0) __syncthreads();
+    if (again) __syncthreads();
+    again = true;
 #pragma unroll
     for (int u = 0; u < kRowsChunk / (64 * N); ++u) {
       const int i = (u * 64 + lane) * N;
@@ -364,10 +375,10 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
   if (held)
     static_for<kRowsHeld / kRowsChunk>([&](auto I) __attribute__((always_inline)) {
       constexpr int c0 = decltype(I)::value * kRowsChunk;
-      if (c0 < dP) chunk(c0, std::integral_constant<int, c0 / (64 * N)>{});
+      if (c0 < dP && decltype(I)::value % splits == split) chunk(c0, std::integral_constant<int, c0 / (64 * N)>{});
     });
   else
-    for (int c0 = 0; c0 < dP; c0 += kRowsChunk) chunk(c0, std::integral_constant<int, -1>{});
+    for (int c0 = split * kRowsChunk; c0 < dP; c0 += splits * kRowsChunk) chunk(c0, std::integral_constant<int, -1>{});
 }
 
 // ---- epilogues -----------------------------------------------------------------------------------------------
@@ -630,8 +641,8 @@ __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restric
   store_result(out, (size_t)m * d + c, out_f32, v * scale);
 }
 
-// Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in their order and hands to the
-// epilogue, a wave 32 rows of 64 columns.
+// Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in an order of their number and
+// hands to the epilogue, a workgroup 32 rows of 64 columns.
 template <int RAW>
 struct EpiPlanes {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -658,34 +669,44 @@ __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restric
   constexpr int PITCH = 68;
   __shared__ __attribute__((aligned(16))) float tiles[4][32 * PITCH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int across = N / 64, id = blockIdx.x * 4 + wave, m0 = id / across * 32, n0 = id % across * 64;
-  if (m0 >= Tp) return;                                              // (whole waves; no barrier follows)
+  const int across = N / 64, m0 = blockIdx.x / across * 32, n0 = blockIdx.x % across * 64;
   Epi epi = epi_in;
-  float* tile = tiles[wave];
   const size_t plane = (size_t)Tp * N;
   const float* p = planes + (size_t)(m0 + (lane >> 4)) * N + n0 + (lane & 15) * 4;
-  f32x4 v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = *(const f32x4*)(p + (size_t)(4 * i) * N);
-  if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
-  for (int s = 1; s < slices; s += 4) {                              // (a slice past the last: the last again, not added)
+  f32x4 v[8] = {};
+  for (int s = wave; s < slices; s += 16) {                          // every fourth slice a wave, four at a time
     f32x4 u[4][8];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[j][i] = *(const f32x4*)(p + min(s + j, slices - 1) * plane + (size_t)(4 * i) * N);
+      for (int i = 0; i < 8; ++i)
+        if (s + 4 * j < slices) u[j][i] = *(const f32x4*)(p + (s + 4 * j) * plane + (size_t)(4 * i) * N);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (s + j < slices) {
+      if (s + 4 * j < slices) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += u[j][i];
       }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) *(f32x4*)(tile + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4) = v[i];
+  for (int i = 0; i < 8; ++i) *(f32x4*)(tiles[wave] + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4) = v[i];
+  if (wave < 2) {
+    if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
+  }
+  __syncthreads();
+  if (wave >= 2) return;
+  float* tile = tiles[0] + wave * 16 * PITCH;                        // 16 rows each of two waves
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float* x = tile + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4;
+    f32x4 y = *(const f32x4*)x;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) y += *(const f32x4*)(x + w * 32 * PITCH);
+    *(f32x4*)x = y;
+  }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __builtin_amdgcn_wave_barrier();
-  epi.template consume<64, PITCH, 32>(tile, m0, n0, lane, M);
+  epi.template consume<64, PITCH, 16>(tile, m0 + wave * 16, n0, lane, M);
 }
 
 // grad_head: rows of a piece of the vocabulary.
@@ -718,16 +739,16 @@ struct EpiHead {
 };
 
 // grad_head of at most 128 rows (bfloat16), where it is bound by what it writes: 64 rows of the head by 64 columns at a time a
-// wave, whose dz stays in registers while it walks 512 columns, straight from the accumulators.  The products are transposed (a row
+// wave, whose dz stays in registers while it walks `walk` columns, straight from the accumulators.  The products are transposed (a row
 // of dz^T is a column here), and which columns of h a tile's rows are is chosen so that a lane holds eight in a row of each two
 // tiles, and the four groups of lanes 64 bytes.
 template <int KS>
 __global__ __launch_bounds__(256) void loss_head_rows_kernel(const f16* __restrict__ dzT, const f16* __restrict__ hT, int Tp,
                                                              const float* __restrict__ dz_max, int n_max, bf16* __restrict__ out,
-                                                             int rows, int d) {
+                                                             int rows, int d, int walk) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = lane >> 4, i = lane & 15, across = (d + 511) / 512, id = blockIdx.x * 4 + wave;
-  const int v0 = id / across * 64, c_first = id % across * 512;
+  const int g = lane >> 4, i = lane & 15, across = (d + walk - 1) / walk, id = blockIdx.x * 4 + wave;
+  const int v0 = id / across * 64, c_first = id % across * walk;
   if (v0 >= rows) return;                                            // (no barriers)
   const size_t k_at = (size_t)(g >> 1) * 512 + (g & 1) * 256;        // of a k-step of 32: group g has k 8 g ..
   f16x8 b[4][KS];
@@ -745,7 +766,7 @@ __global__ __launch_bounds__(256) void loss_head_rows_kernel(const f16* __restri
       for (int ks = 0; ks < KS; ++ks) a[mt][ks] = *(const f16x8*)(hT + (size_t)(c >> 5) * 32 * Tp + ks * 1024 + k_at + (c & 31) * 8);
     }
   };
-  const int c_end = min(c_first + 512, d);
+  const int c_end = min(c_first + walk, d);
   f16x8 a[2][4][KS];
   load(a[0], c_first);
   auto columns = [&](f16x8 (&now)[4][KS], f16x8 (&next)[4][KS], int c0) __attribute__((always_inline)) {
@@ -830,7 +851,8 @@ static int tile_up(int x) { return x <= 128 ? 128 : round_up(x, 256); }        /
 //   (64x128; 128x128 25, 256x256 68);
 //   grad_head 32000 x 4096 x 64 81 (192x256; 128x256 96, 128x128 128), x 4096 814 (256x256; 833, 903);
 //   grad_hidden 2048 x 4096 x 32000 in one slice 407 (128x256; 192x256 467, 256x256 557 of 128 tiles), in two of 256x256 365.
-// Unpacked weights cost 1.35 to 1.5 times the products (re-encoding) and have no 256x256 tile (registers).
+// Unpacked weights cost 1.5 times the products on a full chip (re-encoding), twice on an empty one (the latency of pieces of 128
+// bytes), and have no 256x256 tile (registers).
 enum LossTile { L_64x128, L_64x128_PAIR, L_128x128, L_128x256, L_192x256, L_256x256, L_COUNT };
 enum LossWork { L_STATS, L_DZ, L_STORE };
 struct LossTileCost { int bm, bn, slots; float few, full, fixed[3]; };
@@ -843,7 +865,7 @@ static float launch_us(int t, LossWork work, int M, int N, int K, int slices, bo
   const LossTileCost& c = kLossTiles[t];
   const long long wgs = (long long)((M + c.bm - 1) / c.bm) * (N / c.bn) * slices;
   const float k = (float)round_up(K / slices, PK) / 1024.0f;
-  float few = raw ? c.few * 1.35f : c.few, full = raw ? c.full * 1.5f : c.full;
+  float few = raw ? c.few * 2.0f : c.few, full = raw ? c.full * 1.5f : c.full;
   if ((long long)K * (M > N ? M : N) > 64'000'000) few = fmaxf(few, (float)(c.bm + c.bn) * 2048.0f / 65e3f), full = fmaxf(full, few);
   const float rounds = (float)(wgs / c.slots), rest = (float)(wgs % c.slots) / (float)c.slots;
   return 2.0f + rounds * (c.fixed[work] + full * k) + (rest > 0.f ? c.fixed[work] + (few + (full - few) * rest) * k : 0.f);
@@ -1085,13 +1107,14 @@ RowTargets prepare(const Plan& w, const vla_head_rows& r, const Targets& t, cons
     attr_set = true;
   }
   HeadPack<T> head{};
-  int wgs = w.Tp / 8;
+  const int chunks = (w.dP + kRowsChunk - 1) / kRowsChunk, splits = w.Tp / 8 * chunks <= 1024 ? chunks : 1;
+  int wgs = w.Tp / 8 * splits;
   if (!w.raw && w.pieces == 1) {
     head = head_pack<T>(w, r, 0, w.Vp, w_transposed, work);
     wgs += (w.dP / 64) * (w.Vp / 64) / 2;                            // (columns in pairs of tiles: dP and Vp are multiples of 128)
   }
   hipLaunchKernelGGL(kern, dim3(wgs), dim3(512), (size_t)96 * ((w.k + 3) & ~3), st, (const T*)r.hidden, r.ld_hidden, w.T, w.d, w.V,
-                     1.0f / tau, t.labels, t.top_logits, t.top_ids, w.k, w.groups, g, w.Tp, w.dP, out, head);
+                     1.0f / tau, t.labels, t.top_logits, t.top_ids, w.k, w.groups, g, w.Tp, w.dP, splits, out, head);
   return RowTargets{out.z_scale, w.k ? nullptr : out.label, out.ids, out.p, out.first, w.k, w.groups};
 }
 
@@ -1114,7 +1137,7 @@ void logits(const Plan& w, const LossPick& pick, const vla_head_rows& r, int n0,
     const auto epi = make(RAW);
     if (pick.slices == 1) return product(pick.tile, hF, ld, W, w.T, N, K, epi, st);
     if (!have_planes) product(pick.tile, hF, ld, W, w.T, N, K, EpiPlanes<raw>{pick.slices, zp, w.Tp, N, r.ld_head, rows}, st);
-    hipLaunchKernelGGL((loss_slices_kernel<std::remove_const_t<decltype(epi)>>), dim3(((w.Tp / 32) * (N / 64) + 3) / 4), dim3(256), 0, st,
+    hipLaunchKernelGGL((loss_slices_kernel<std::remove_const_t<decltype(epi)>>), dim3((w.Tp / 32) * (N / 64)), dim3(256), 0, st,
                        zp, pick.slices, w.Tp, N, w.T, epi);
   };
   if constexpr (std::is_same_v<T, bf16>) {
@@ -1187,9 +1210,11 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
                 EpiHidden<2>{w.hidden.slices, set, add, w.T, w.dP, f(w.coef), gh, 0, w.d, r.ld_head, rows, w.d}, st);
     if (!w.raw && gh) product(w.hidden.tile, dzF, K, work + w.wT, w.T, w.dP, K, hidden, st);
     if (gw && !f32 && w.Tp <= 128) {
-      const dim3 grid((unsigned)(((rows + 63) / 64) * ((w.d + 511) / 512) + 3) / 4);
+      int walk = 512;                                                // (1024 waves, if there are as many)
+      while (walk > 64 && (long long)((rows + 63) / 64) * ((w.d + walk - 1) / walk) < 1024) walk /= 2;
+      const dim3 grid((unsigned)(((rows + 63) / 64) * ((w.d + walk - 1) / walk) + 3) / 4);
       auto kern = w.Tp == 64 ? loss_head_rows_kernel<2> : loss_head_rows_kernel<4>;
-      hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, dzT, h(w.hT), w.Tp, f(w.dz_max), n_max, (bf16*)gw + (size_t)n0 * w.d, rows, w.d);
+      hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, dzT, h(w.hT), w.Tp, f(w.dz_max), n_max, (bf16*)gw + (size_t)n0 * w.d, rows, w.d, walk);
       continue;
     }
     if (gw) product(w.head.tile, dzT, K2, h(w.hT), N, w.dP, K2, head, st);
