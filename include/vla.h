@@ -265,6 +265,13 @@ int vla_score_tokens(vla_ctx* ctx, int32_t B, const void* patch_emb, const int32
                      int32_t placeholder_id, float temperature, const float* mu_logp, float sigma,
                      float* logp_out, float* ratio_out, float* weight_out, float* logits_out, void* hip_stream);
 
+/* The rows behind the logits of the vla_score_tokens or vla_policy_step_parallel call that came directly before (no other compute
+ * call and no load or update in between, else VLA_E_STATE; B and n_tokens as in that call): hidden_out, device, [B, K, d_model] in
+ * the storage dtype, starting on 16 bytes, is the final norm's output at the positions that emit the action tokens.  With the rows of
+ * the action bins of lm_head it gives those logits (up to the rounding to the storage dtype; the call itself keeps float32), and
+ * the losses of vla_loss.h take both. */
+int vla_action_hidden(vla_ctx* ctx, int32_t B, int32_t n_tokens, void* hidden_out, void* hip_stream);
+
 /* Continuous batching: the same two steps on an arbitrary set of cache slots, so that newly admitted requests are
  * prefilled while the sequences already running keep decoding in shared steps.  Sequence i of a call lives in
  * cache slot slot_ids[i] (host array, n distinct values in [0, max_batch)); rows of patch_emb / offsets /

@@ -12,6 +12,7 @@ from .binding import (  # noqa: F401
     VLA_ACCEPTING, VLA_DRAINING, VLA_UPDATING, VLA_E_STATE, VLA_E_DRAINING,
     vla_prof_enable, vla_prof_count, vla_prof_read, vla_probe,
     vla_head_rows, vla_loss_workspace, vla_token_loss, vla_token_loss_grad, vla_distill_loss, vla_distill_loss_grad,
+    vla_action_hidden,
 )
 from .losses import distill_loss, distill_loss_grad, token_loss, token_loss_grad  # noqa: F401,E402
 from .serving import ContinuousWorker, InferenceWorker  # noqa: F401,E402

@@ -25,7 +25,8 @@ EXPORTS = ["vla_create", "vla_destroy", "vla_last_error", "vla_query_sizes", "vl
            "vla_batcher_deadline", "vla_batcher_poll",
            "vla_get_state", "vla_drain_begin", "vla_update_begin", "vla_update_tensors", "vla_update_commit",
            "vla_prof_enable", "vla_prof_count", "vla_prof_read",
-           "vla_loss_workspace", "vla_token_loss", "vla_token_loss_grad", "vla_distill_loss", "vla_distill_loss_grad"]
+           "vla_loss_workspace", "vla_token_loss", "vla_token_loss_grad", "vla_distill_loss", "vla_distill_loss_grad",
+           "vla_action_hidden"]
 
 
 class vla_config(C.Structure):
@@ -96,6 +97,7 @@ def lib() -> C.CDLL:
         L.vla_update_commit.argtypes = [vp, vp, C.POINTER(C.c_int64)]
         L.vla_policy_step_parallel.argtypes = [vp, i32, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
         L.vla_score_tokens.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, f32, vp, f32, vp, vp, vp, vp, vp]
+        L.vla_action_hidden.argtypes = [vp, i32, i32, vp, vp]
         L.vla_prefill_slots.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp]
         L.vla_decode_slots.argtypes = [vp, i32, vp, vp, vp, vp]
         L.vla_release_slots.argtypes = [vp, i32, vp]
@@ -246,6 +248,10 @@ def vla_score_tokens(ctx, B, patch_emb, cu_patch, instr_ids, cu_instr, n_tokens,
     _check(ctx, lib().vla_score_tokens(ctx, B, _ptr(patch_emb), _ptr(cu_patch), _ptr(instr_ids), _ptr(cu_instr),
                                        n_tokens, _ptr(tokens), placeholder_id, temperature, _ptr(mu_logp), sigma,
                                        _ptr(logp_out), _ptr(ratio_out), _ptr(weight_out), _ptr(logits_out), stream))
+
+
+def vla_action_hidden(ctx, B: int, n_tokens: int, hidden_out, stream: int = 0) -> None:
+    _check(ctx, lib().vla_action_hidden(ctx, B, n_tokens, _ptr(hidden_out), stream))
 
 
 def vla_prefill_slots(ctx, slot_ids, patch_emb, cu_patch, instr_ids, cu_instr, logits_out, stream: int = 0) -> None:
@@ -558,6 +564,14 @@ class VlaPolicy:
                          np.ascontiguousarray(cu_instr, dtype=np.int32), K, tokens, int(placeholder_id),
                          float(temperature), mu_logp, float(sigma), out["logp"], out["ratio"], out["weight"],
                          out["logits"], self._stream())
+        return out
+
+    def action_hidden(self, B: int, n_tokens: int):
+        """[B * K, d_model] rows that the head took in the score_tokens / policy_step_parallel call directly before; with the
+        action rows of lm_head they go into token_loss and distill_loss."""
+        out = self.torch.empty((B * n_tokens, self.shape.d_model), device=self.device,
+                               dtype=self.torch.bfloat16 if self.dtype_code == VLA_BF16 else self.torch.float32)
+        vla_action_hidden(self.ctx, B, n_tokens, out, self._stream())
         return out
 
     def policy_step(self, patch_emb, cu_patch, instr_ids, cu_instr, n_tokens, temperature=0.0, gumbel=None,

@@ -232,6 +232,7 @@ struct vla_ctx {
   hipEvent_t ev_update = nullptr;    // recorded when the last load / update was committed, on its stream
   bool have_work = false, have_update = false;
   int active_B = 0;                  // batch of the last prefill (0: none)
+  int chunk_B = 0, chunk_K = 0;      // of the one-pass call whose rows are still in the workspace (0: none)
   int run_B = 0, run_max_len = 0;    // batch and longest prefix of the prefill being enqueued
   const int32_t* run_slots = nullptr; // device slot map of the call being enqueued (nullptr: sequence b is slot b)
   float* part_override = nullptr;    // set for the duration of vla_decode_step_static: GEMM staging outside the workspace
@@ -708,6 +709,7 @@ int check_serving(vla_ctx* ctx, bool new_batch) {
 }
 
 int enter_compute(vla_ctx* ctx, hipStream_t st) {
+  ctx->chunk_B = 0;                  // the workspace is about to be overwritten
   if (ctx->have_update) HIP_TRY(ctx, hipStreamWaitEvent(st, ctx->ev_update, 0));
   return VLA_OK;
 }
@@ -885,6 +887,8 @@ int do_chunk(vla_ctx* ctx, int32_t B, const void* patch_emb, const int32_t* cu_p
   const int32_t* rows = K > 1 ? at<int32_t>(ctx->work, w.chunk_rows) : at<int32_t>(ctx->work, w.last_row);
   run_head<T>(ctx, B * K, rows, logits, A, st);
   HIP_TRY(ctx, hipGetLastError());
+  ctx->chunk_B = B;
+  ctx->chunk_K = K;
   return VLA_OK;
 }
 
@@ -986,6 +990,7 @@ int vla_bind_buffers(vla_ctx* ctx, void* weight_arena, void* kv, void* workspace
   ctx->weights = false;
   ctx->value_weights = false;
   ctx->tables = false;
+  ctx->chunk_B = 0;
   ctx->active_B = 0;
   ctx->len.assign(ctx->cfg.max_batch, 0);
   ctx->serving = VLA_ACCEPTING;
@@ -1143,6 +1148,7 @@ int load_slots(vla_ctx* ctx, const std::vector<const vla_tensor*>& slot, bool wh
   HIP_TRY(ctx, hipEventRecord(ctx->ev_update, st));
   ctx->have_update = true;
   ctx->version += 1;
+  ctx->chunk_B = 0;
   ctx->active_B = 0;     // cached keys / values belong to the old weights
   ctx->len.assign(ctx->cfg.max_batch, 0);
   return VLA_OK;
@@ -1213,6 +1219,7 @@ int vla_update_begin(vla_ctx* ctx, void* hip_stream) {
   if (ctx->serving == VLA_UPDATING) return fail(ctx, VLA_E_DRAINING, "an update is already open");
   if (ctx->have_work) HIP_TRY(ctx, hipStreamWaitEvent((hipStream_t)hip_stream, ctx->ev_work, 0));
   ctx->serving = VLA_UPDATING;
+  ctx->chunk_B = 0;
   ctx->active_B = 0;     // the batch in flight has been enqueued to its end; its cache dies with the old weights
   ctx->len.assign(ctx->cfg.max_batch, 0);
   return VLA_OK;
@@ -1524,6 +1531,30 @@ int vla_score_tokens(vla_ctx* ctx, int32_t B, const void* patch_emb, const int32
   {
     ProfScope ps(ctx, FAM_HEAD, st);
     score_rows(lg, B * K, A, temperature, tokens, mu_logp, sigma, logp_out, ratio_out, weight_out, st);
+  }
+  HIP_TRY(ctx, hipGetLastError());
+  return leave_compute(ctx, st);
+}
+
+int vla_action_hidden(vla_ctx* ctx, int32_t B, int32_t n_tokens, void* hidden_out, void* hip_stream) {
+  if (!ctx) return VLA_E_NULL;
+  int rc = check_ready(ctx);
+  if (rc) return rc;
+  if ((rc = check_serving(ctx, false))) return rc;
+  if (!hidden_out) return fail(ctx, VLA_E_NULL, "hidden_out is NULL");
+  if ((uintptr_t)hidden_out & 15) return fail(ctx, VLA_E_SHAPE, "hidden_out must start on 16 bytes");
+  if (ctx->chunk_B == 0) return fail(ctx, VLA_E_STATE, "no rows: vla_score_tokens or vla_policy_step_parallel comes directly before");
+  if (B != ctx->chunk_B || n_tokens != ctx->chunk_K)
+    return fail(ctx, VLA_E_SHAPE, "%d x %d rows asked for, the last call had %d x %d", B, n_tokens, ctx->chunk_B, ctx->chunk_K);
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (ctx->have_update) HIP_TRY(ctx, hipStreamWaitEvent(st, ctx->ev_update, 0));
+  const vla_config& c = ctx->cfg;
+  const int32_t* rows = n_tokens > 1 ? at<int32_t>(ctx->work, ctx->wl.chunk_rows) : at<int32_t>(ctx->work, ctx->wl.last_row);
+  const float *x = at<float>(ctx->work, ctx->wl.x), *gain = at<float>(ctx->arena, ctx->al.g_final);
+  {
+    ProfScope ps(ctx, FAM_HEAD, st);
+    if (c.dtype == VLA_BF16) action_hidden<bf16>(x, rows, gain, (bf16*)hidden_out, B * n_tokens, c.d_model, c.rms_eps, st);
+    else action_hidden<float>(x, rows, gain, (float*)hidden_out, B * n_tokens, c.d_model, c.rms_eps, st);
   }
   HIP_TRY(ctx, hipGetLastError());
   return leave_compute(ctx, st);

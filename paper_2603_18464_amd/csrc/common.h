@@ -294,6 +294,9 @@ void decode_attention_fused(const float* part, int ksplit, int part_rows, const 
 template <class T>
 void head_logits(const float* x, const int32_t* row_index, const float* gain, const T* w_head,
                  float* logits, int ld_logits, int B, int d, int A, float eps, hipStream_t st);
+// The rows of x that row_index lists after the final norm, as the head takes them, in the storage type.
+template <class T>
+void action_hidden(const float* x, const int32_t* row_index, const float* gain, T* out, int rows, int d, float eps, hipStream_t st);
 void select_tokens(const float* logits, int ld_logits, int B, int A, float temperature, const float* gumbel, int k,
                    int n_tokens, const float* act_scale, const float* act_offset, int action_dim,
                    int32_t* tokens_out, float* logp_out, float* actions_out, int out_stride,

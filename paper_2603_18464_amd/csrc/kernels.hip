@@ -487,6 +487,37 @@ template void head_logits<float>(const float*, const int32_t*, const float*, con
 template void head_logits<bf16>(const float*, const int32_t*, const float*, const bf16*, float*, int, int, int,
                                 int, float, hipStream_t);
 
+// The rows that head_kernel multiplies, for a learner's losses: the same norm, rounded to the storage type.  A row a workgroup;
+// bound by its launch (some hundred rows of 16 KB).
+template <class T>
+__global__ __launch_bounds__(256) void action_hidden_kernel(const float* __restrict__ x, const int32_t* __restrict__ row_index,
+                                                            const float* __restrict__ gain, T* __restrict__ out, int d, float eps) {
+  __shared__ float red[4];
+  const float* row = x + (size_t)row_index[blockIdx.x] * d;
+  float ss = 0.f;
+  for (int i = threadIdx.x * 4; i < d; i += 1024) {
+    const float4 v = *(const float4*)(row + i);
+    ss += v.x * v.x + v.y * v.y + v.z * v.z + v.w * v.w;
+  }
+  ss = block_sum_256(ss, red);
+  const float inv = 1.0f / sqrtf(ss / (float)d + eps);
+  T* o = out + (size_t)blockIdx.x * d;
+  for (int i = threadIdx.x * 4; i < d; i += 1024) {
+    const float4 v = *(const float4*)(row + i);
+    const float4 g = *(const float4*)(gain + i);
+    o[i] = from_f32<T>(v.x * inv * g.x);
+    o[i + 1] = from_f32<T>(v.y * inv * g.y);
+    o[i + 2] = from_f32<T>(v.z * inv * g.z);
+    o[i + 3] = from_f32<T>(v.w * inv * g.w);
+  }
+}
+template <class T>
+void action_hidden(const float* x, const int32_t* row_index, const float* gain, T* out, int rows, int d, float eps, hipStream_t st) {
+  hipLaunchKernelGGL((action_hidden_kernel<T>), dim3(rows), dim3(256), 0, st, x, row_index, gain, out, d, eps);
+}
+template void action_hidden<float>(const float*, const int32_t*, const float*, float*, int, int, float, hipStream_t);
+template void action_hidden<bf16>(const float*, const int32_t*, const float*, bf16*, int, int, float, hipStream_t);
+
 // ---- value head ---------------------------------------------------------------------------------------
 // Action-aware attention pooling over the K hidden rows that feed the action head, done online: after
 // each head evaluation the row's score e = w_attn . h + b_attn updates a running softmax-weighted sum

@@ -120,3 +120,13 @@ def test_tensors_that_are_refused():
         with pytest.raises(P.VlaError) as e:                             # (the last: not on a GPU)
             P.token_loss(hh, ww, y)
         assert e.value.code == code
+
+
+def test_rows_of_a_context_without_a_call():
+    import workloads as W
+    wl = W.get_workload("C1")
+    L = B.lib()
+    assert L.vla_action_hidden(None, 1, 1, 256, None) == -1
+    ctx = B.vla_create(B.make_config(wl.shape, 4, 64, 256))
+    assert L.vla_action_hidden(ctx, 1, 1, 256, None) == -5               # nothing is bound
+    B.vla_destroy(ctx)
