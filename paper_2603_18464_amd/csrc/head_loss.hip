@@ -1,9 +1,10 @@
 // The head's losses (include/vla_loss.h): cross entropy of tokens and distillation from a teacher's top logits, with their
 // gradients.  Both are one thing: a row's target is a short sorted list of (id, probability), one entry for a token.
 //
-// Mathematics.  With z = h W^T / tau in base-e logits, a group of 64 columns of a row leaves (m, l, a) = (max z, sum exp(z - m),
-// sum over the row's entries in the group of p z); the groups are joined in their order to lse = m + log l, and
-//     loss = sum p log p + (sum p) lse - sum p z        (a token: lse - z_label).
+// Mathematics.  With z = h W^T / tau, a group of 64 columns of a row leaves m = max z and l = sum exp(z - m), the groups are joined
+// in a fixed order, and
+//     lse = m + log l,   loss = log l + (m - z_label)   (lists: sum p log p + (sum p) lse - sum p z).
+// float32 carries t = l - 1, the sum without the largest, in place of l: a row that is sure of its token has nothing but t.
 // The gradient forms z again, dz = q - r with q = exp(z - lse), and two products: grad_hidden = (g / tau) dz W, where a row's
 // coefficient is applied at the end, and grad_head = dz^T (g h / tau), where it is applied to h.
 //
@@ -12,7 +13,8 @@
 // [-1, 1], by 2^15 for grad_hidden, whose rows take their g / tau at the end, and times g / tau over the row's scale as one tensor
 // to a maximum of 2^15 for grad_head.  dz is rounded to half precision (2^-11 of its value at most); everything else is float32.
 // float32 operands are carried as two terms hi + lo (22 bits); a product of two of them is three, hi hi + lo hi + hi lo,
-// laid out as one contraction three times as long: [hi | lo | hi] against [hi | hi | lo].
+// laid out as one contraction three times as long: [lo | hi | hi] against [hi | lo | hi], the small products first, so that their
+// sums are rounded at their own size.
 //
 // What bounds them: the large calls by the matrix cores (2 T V d operations forward, 6 backward).
 #include "gemm_tile.h"
@@ -82,7 +84,7 @@ __device__ __forceinline__ float head_scale(const float* dz_max, int n, int lane
 }
 
 // The head where it is not read as it is: 64 x 64 elements of src [R, C] by 256 threads, as rows (F [Rp, Cp], contraction over
-// the columns) and transposed (FT [Cp, Rp], or nullptr), zeros past R and C.  TERMS 3: [hi | hi | lo], a third of the contraction
+// the columns) and transposed (FT [Cp, Rp], or nullptr), zeros past R and C.  TERMS 3: [hi | lo | hi], a third of the contraction
 // each.
 template <class T>
 struct HeadPack {
@@ -113,8 +115,8 @@ __device__ __forceinline__ void pack_tile(const HeadPack<T>& h, int tile_id, int
       f16x8 lo;
 #pragma unroll
       for (int j = 0; j < 8; ++j) lo[j] = from_f32<f16>(x[j] - (float)hi[j]);
-      *(f16x8*)(dst + act_index(m, third + kk, 3 * third)) = hi;
-      *(f16x8*)(dst + act_index(m, 2 * third + kk, 3 * third)) = lo;
+      *(f16x8*)(dst + act_index(m, third + kk, 3 * third)) = lo;
+      *(f16x8*)(dst + act_index(m, 2 * third + kk, 3 * third)) = hi;
     }
   };
   if (r < h.Rp) {
@@ -351,10 +353,10 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
     for (int i = threadIdx.x; i < n; i += 512) {                     // rows: 8 of a chunk of 8 columns side by side
       const int r = i & 7, c = i & ~7;
       const f16x8 hi = *(const f16x8*)(&tile[0][r * PITCH + c]);
-      *(f16x8*)(out.F + act_index(row0 + r, c0 + c, ldF)) = hi;
+      *(f16x8*)(out.F + act_index(row0 + r, (TERMS - 1) * dP + c0 + c, ldF)) = hi;
       if constexpr (TERMS == 3) {
-        *(f16x8*)(out.F + act_index(row0 + r, dP + c0 + c, ldF)) = *(const f16x8*)(&tile[TERMS == 3][r * PITCH + c]);
-        *(f16x8*)(out.F + act_index(row0 + r, 2 * dP + c0 + c, ldF)) = hi;
+        *(f16x8*)(out.F + act_index(row0 + r, c0 + c, ldF)) = *(const f16x8*)(&tile[TERMS == 3][r * PITCH + c]);
+        *(f16x8*)(out.F + act_index(row0 + r, dP + c0 + c, ldF)) = hi;
       }
     }
     if (out.FT)
@@ -367,8 +369,8 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
         }
         *(f16x8*)(out.FT + act_index(c0 + i, row0, ldT)) = hi;
         if constexpr (TERMS == 3) {
-          *(f16x8*)(out.FT + act_index(c0 + i, Tp + row0, ldT)) = hi;
-          *(f16x8*)(out.FT + act_index(c0 + i, 2 * Tp + row0, ldT)) = lo;
+          *(f16x8*)(out.FT + act_index(c0 + i, Tp + row0, ldT)) = lo;
+          *(f16x8*)(out.FT + act_index(c0 + i, 2 * Tp + row0, ldT)) = hi;
         }
       }
   };
@@ -384,11 +386,12 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
 // ---- epilogues -----------------------------------------------------------------------------------------------
 // Partial statistics of the groups of 64 columns.  ROWS rows of a group by 64 / ROWS lanes each; a group's sums are formed in
 // the same order whatever the tile, so a row's loss does not depend on the rows beside it.
-template <int RAW>
+// EXACT (float32): t in place of l, from differences to the largest that are exact where they are small.
+template <int RAW, bool EXACT>
 struct EpiStats {
   static constexpr int kSpan = 64, kRaw = RAW;
   RowTargets tg;
-  float *pm, *pl;            // [groups][T]
+  float *pm, *pl;            // [groups][T] m and l (t) of a group
   float* pa;                 // z of the label [T], or p z of the entries [T][k]
   int T, V, n_base;          // first column of the launch
   int64_t raw_ld;
@@ -408,10 +411,10 @@ struct EpiStats {
       float x[W];
 #pragma unroll
       for (int i = 0; i < W; i += 4) *(f32x4*)(x + i) = *(const f32x4*)(tile + r * PITCH + c0 + i);
-      // An infinite weight makes infinite products, which as -inf would count as probabilities of 0: `odd` is a NaN then.
-      float odd = 0.f;
+      // An infinite weight makes infinite products, which as -inf would count as probabilities of 0: a NaN then.
+      float mn = INFINITY;
 #pragma unroll
-      for (int i = 0; i < W; ++i) odd = fmaf(x[i], 0.f, odd);
+      for (int i = 0; i < W; ++i) mn = fminf(mn, x[i]);
       if (n0 + kGroup > V) {                             // (uniform) the last group
 #pragma unroll
         for (int i = 0; i < W; ++i) x[i] = i < left ? x[i] : -INFINITY;
@@ -420,19 +423,27 @@ struct EpiStats {
 #pragma unroll
       for (int i = 0; i < W; ++i) mx = fmaxf(mx, x[i]);
       mx = lanes_max<ROWS, 32>(mx);
-      const float z2 = zs * kLog2e, ref2 = mx == -INFINITY ? 0.f : -mx * z2;
+      const float z2 = zs * kLog2e, ref = mx == -INFINITY ? 0.f : mx, ref2 = -ref * z2;
       float l = 0.f;                                     // sums of 16 columns, joined in pairs
+      int ties = 0;                                      // of the largest
 #pragma unroll
       for (int h = 0; h < W / 16; ++h) {
         float s4[4] = {};
 #pragma unroll
         for (int i = 16 * h; i < 16 * h + 16; ++i) {
-          s4[i & 3] += __builtin_amdgcn_exp2f(fmaf(x[i], z2, ref2));
+          if constexpr (EXACT) {
+            const float e = __builtin_amdgcn_exp2f((x[i] - ref) * z2);
+            ties += x[i] == mx;
+            s4[i & 3] += x[i] == mx ? 0.f : e;
+          } else {
+            s4[i & 3] += __builtin_amdgcn_exp2f(fmaf(x[i], z2, ref2));
+          }
         }
         l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
       }
-      l += odd;
+      if (mn == -INFINITY) l = NAN;
       l = lanes_sum<ROWS, 32>(l);
+      if constexpr (EXACT) l += lanes_sum<ROWS, 32>((float)ties) - 1.0f;
       if (part == 0 && m < M && n0 < V) {
         if (tg.label) {
           const int c = label - n0;
@@ -451,13 +462,20 @@ struct EpiStats {
   }
 };
 
+// z - m with z rounded as it was for m: of the largest 0, which a fused multiply-subtract would miss by the rounding.
+__device__ __forceinline__ float from_largest(float x, float z_scale, float m) {
+#pragma clang fp contract(off)
+  const float z = x * z_scale;
+  return z - m;
+}
 // dz as the operand of both gradient products: rows (F, times 2^15) and transposed (FT, times the rows' coefficients and what
 // brings them all to 2^15).  Rows T .. Tp and columns V .. are zeros.
 template <int RAW, int TERMS>
 struct EpiDz {
   static constexpr int kSpan = 64, kRaw = RAW;
   RowTargets tg;
-  const float* lse;
+  const float* lse;          // float32: t of the row, with its m in ref
+  const float* ref;
   const float *dz_coef, *dz_max;
   int n_max;
   f16 *F, *FT;
@@ -472,13 +490,13 @@ struct EpiDz {
     f16x8 hi;
 #pragma unroll
     for (int j = 0; j < 8; ++j) hi[j] = from_f32<f16>(x[j]);
-    *(f16x8*)dst = hi;
+    *(f16x8*)(dst + (TERMS - 1) * third) = hi;
     if constexpr (TERMS == 3) {
       f16x8 lo;
 #pragma unroll
       for (int j = 0; j < 8; ++j) lo[j] = from_f32<f16>(x[j] - (float)hi[j]);
-      *(f16x8*)(dst + third) = lo;
-      *(f16x8*)(dst + 2 * third) = hi;
+      *(f16x8*)dst = lo;
+      *(f16x8*)(dst + third) = hi;
     }
   }
   template <int COLS, int PITCH, int ROWS>
@@ -488,7 +506,12 @@ struct EpiDz {
     const int r = lane % ROWS, part = lane / ROWS, m = m_base + r, mc = min(m, M - 1);
     // dz * 2^15; a row without target, and one past the last: zeros.  (A head that half precision does not hold has made lse a NaN.)
     const bool live = m < M && tg.z_scale[mc] != 0.f;
-    const float z2 = live ? tg.z_scale[mc] * kLog2e : 0.f, ref2 = live ? fmaf(-lse[mc], kLog2e, 15.0f) : -INFINITY;
+    // float32: q = exp(z - m) / (1 + t) from the statistics of these very logits; the largest one's distance from 1, which is all
+    // there is of a row that is sure of its token, is -t / (1 + t).
+    constexpr bool own = TERMS == 3;
+    const float zs = live ? tg.z_scale[mc] : 0.f, z2 = zs * kLog2e, stat = lse[mc];
+    const float ref2 = !live ? (own ? INFINITY : -INFINITY) : own ? ref[mc] : fmaf(-stat, kLog2e, 15.0f);
+    const float scale = own && live ? kDzScale / (1.0f + stat) : 0.f, top = -stat * scale;
     const float ft = live ? dz_coef[mc] * ft_scale : 0.f;
     static_assert(kDzScale == 32768.0f, "2^15");
     const int label = tg.label ? tg.label[mc] : -1;
@@ -516,11 +539,18 @@ struct EpiDz {
       float* x = tile + r * PITCH + c;
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __builtin_amdgcn_exp2f(fmaf(x[j], z2, ref2));
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (own) v[j] = __builtin_amdgcn_exp2f(from_largest(x[j], zs, ref2) * kLog2e) * scale;
+        else v[j] = __builtin_amdgcn_exp2f(fmaf(x[j], z2, ref2));
+      }
       if (tg.label) {
         if ((unsigned)(label - n) < 8u) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] -= n + j == label ? kDzScale : 0.f;
+          for (int j = 0; j < 8; ++j) {
+            if (n + j != label) continue;
+            if constexpr (own) v[j] = v[j] == scale ? top : v[j] - kDzScale;
+            else v[j] -= kDzScale;
+          }
         }
         finish(x, v, it, c);
       } else {                                           // lists: the entries are taken off in the LDS
@@ -535,7 +565,8 @@ struct EpiDz {
         for (int e = entry[0]; e < entry[COLS / kGroup]; ++e) {
           const size_t at = (size_t)m * tg.k + e;
           float* x = &tile[r * PITCH + tg.ids[at] - n_base - nb];
-          *x = fmaf(tg.p[at], -kDzScale, *x);
+          if constexpr (own) *x = *x == scale ? fmaf(1.0f - tg.p[at], kDzScale, top) : fmaf(tg.p[at], -kDzScale, *x);
+          else *x = fmaf(tg.p[at], -kDzScale, *x);
         }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
       __builtin_amdgcn_wave_barrier();
@@ -912,19 +943,26 @@ static void gradients(const f16* A, int lda, const f16* W, int M, int N, int K, 
 }
 
 // ---- joining the groups -------------------------------------------------------------------------------------------
-// 16 rows a workgroup, 64 threads a row, which take every 64th group; their sums are joined in a tree.
+// (EXACT as above.)  16 rows a workgroup, 64 threads a row, which take every 64th group; their sums are joined in a tree.
+template <bool EXACT>
 __global__ __launch_bounds__(1024) void loss_join_kernel(const float* __restrict__ pm, const float* __restrict__ pl,
                                                          const float* __restrict__ pa, int T, int groups, RowTargets tg,
                                                          const float* __restrict__ ent, const float* __restrict__ mass,
-                                                         float* __restrict__ loss, float* __restrict__ lse) {
+                                                         float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ ref_out) {
   __shared__ float sm[64][17], sl[64][17], sa[64][17];
   const int r = threadIdx.x & 15, part = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
   const bool live = row < T && tg.z_scale[row] != 0.f;
   float m = -INFINITY, l = 0.f, a = 0.f;
   auto add = [](float& m, float& l, float m2, float l2) {            // (m, l) and another one to a common maximum
-    const float mm = fmaxf(m, m2), ref = mm == -INFINITY ? 0.f : mm;
-    l = l * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + l2 * __builtin_amdgcn_exp2f((m2 - ref) * kLog2e);
-    m = mm;
+    if constexpr (EXACT) {
+      if (m2 == -INFINITY) return;                                   // (a part without groups)
+      if (m2 <= m) l += (1.0f + l2) * __builtin_amdgcn_exp2f((m2 - m) * kLog2e);
+      else l = m == -INFINITY ? l2 : l2 + (1.0f + l) * __builtin_amdgcn_exp2f((m - m2) * kLog2e), m = m2;
+    } else {
+      const float mm = fmaxf(m, m2), ref = mm == -INFINITY ? 0.f : mm;
+      l = l * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + l2 * __builtin_amdgcn_exp2f((m2 - ref) * kLog2e);
+      m = mm;
+    }
   };
   if (live) {
     for (int g0 = part; g0 < groups; g0 += 256) {
@@ -956,10 +994,14 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(const float* __restrict
     }
   }
   if (part == 0 && row < T) {
-    // (the difference to the largest logit first: it is exact, and nothing where that is the label's)
-    const float ref = m == -INFINITY ? 0.f : m, lg = logf(l);
-    lse[row] = live ? ref + lg : 0.f;
-    if (loss) loss[row] = !live ? 0.f : tg.label ? lg + (ref - pa[row]) : ent[row] + (mass[row] * lg + fmaf(mass[row], ref, -a));
+    const float ref = m == -INFINITY ? 0.f : m, lg = EXACT ? log1pf(l) : logf(l);
+    if (ref_out) {                                                   // for a gradient: m and t
+      ref_out[row] = live ? ref : 0.f;
+      lse[row] = live ? l : 0.f;
+    } else {                                                         // (the difference to the largest logit first: it is exact)
+      lse[row] = live ? ref + lg : 0.f;
+      loss[row] = !live ? 0.f : tg.label ? lg + (ref - pa[row]) : ent[row] + (mass[row] * lg + fmaf(mass[row], ref, -a));
+    }
   }
 }
 
@@ -975,7 +1017,7 @@ struct Plan {
   LossPick hidden, head;
   int sets;                    // planes of grad_hidden: of each slice, of up to four pieces (later ones add to them)
   size_t z_scale, coef, dz_coef, dz_max, label, ids, p, ent, mass, first;
-  size_t hF, hT, wF, wT, dzF, dzT, planes, head_planes, zp, pm, pl, pa, lse, bytes;
+  size_t hF, hT, wF, wT, dzF, dzT, planes, head_planes, zp, pm, pl, pa, ref, sum, bytes;
 };
 
 Plan make_plan(const vla_head_rows& r, int k, bool grad) {
@@ -1037,7 +1079,7 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
     w.sets = min(w.pieces, 4);
     if (w.sets * w.hidden.slices > 1) w.planes = take(4 * T * w.dP * w.sets * w.hidden.slices);
     if (w.head.slices > 1) w.head_planes = take(4 * (size_t)w.head.slices * w.Vp * w.dP);
-    if (w.terms == 3) w.lse = take(4 * T);
+    if (w.terms == 3) w.ref = take(4 * T), w.sum = take(4 * T);
   }
   w.bytes = at;
   return w;
@@ -1146,25 +1188,26 @@ void logits(const Plan& w, const LossPick& pick, const vla_head_rows& r, int n0,
   run(std::integral_constant<int, 0>{}, ld);
 }
 
-// Statistics of the whole vocabulary, and their sums.
+// Statistics of the whole vocabulary, and what they come to: loss and lse, or (ref) t and m.
 template <class T>
-void statistics(const Plan& w, const vla_head_rows& r, const RowTargets& tg, float* loss, float* lse, char* work, hipStream_t st) {
+void statistics(const Plan& w, const vla_head_rows& r, const RowTargets& tg, float* loss, float* lse, float* ref, char* work,
+                hipStream_t st) {
   auto f = [&](size_t o) { return (float*)(work + o); };
   for (int i = 0; i < w.pieces; ++i) {
     const int n0 = i * w.piece, N = min(w.piece, w.Vp - n0), rows = min(N, w.V - n0);
     if (!w.raw && w.pieces > 1) pack_piece<T>(w, r, n0, N, false, work, st);
     logits<T>(w, w.stats, r, n0, N, rows, false, work, [&](auto RAW) {
-      return EpiStats<decltype(RAW)::value>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, n0, r.ld_head, rows};
+      return EpiStats<decltype(RAW)::value, std::is_same_v<T, float>>{tg, f(w.pm), f(w.pl), f(w.pa), w.T, w.V, n0, r.ld_head, rows};
     }, st);
   }
-  hipLaunchKernelGGL(loss_join_kernel, dim3((w.T + 15) / 16), dim3(1024), 0, st, f(w.pm), f(w.pl), f(w.pa), w.T, w.groups, tg,
-                     f(w.ent), f(w.mass), loss, lse);
+  hipLaunchKernelGGL((loss_join_kernel<std::is_same_v<T, float>>), dim3((w.T + 15) / 16), dim3(1024), 0, st, f(w.pm), f(w.pl), f(w.pa), w.T, w.groups, tg,
+                     f(w.ent), f(w.mass), loss, lse, ref);
 }
 
 template <class T>
 int run_loss(const Plan& w, const vla_head_rows& r, const Targets& t, float* loss, float* lse, char* work, hipStream_t st) {
   const RowTargets tg = prepare<T>(w, r, t, nullptr, false, false, work, st);
-  statistics<T>(w, r, tg, loss, lse, work, st);
+  statistics<T>(w, r, tg, loss, lse, nullptr, work, st);
   return hipGetLastError() == hipSuccess ? VLA_OK : VLA_E_HIP;
 }
 
@@ -1177,8 +1220,8 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
   auto f = [&](size_t o) { return (float*)(work + o); };
   auto h = [&](size_t o) { return (f16*)(work + o); };
   if (f32) {
-    statistics<T>(w, r, tg, nullptr, f(w.lse), work, st);
-    lse = f(w.lse);
+    statistics<T>(w, r, tg, nullptr, f(w.sum), f(w.ref), work, st);
+    lse = f(w.sum);
   }
   const bool have_planes = f32 && w.z.slices > 1;                    // (of the logits, from their statistics)
   int n_max = w.Tp / 8;
@@ -1194,7 +1237,7 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
     f16 *dzF = gh ? h(w.dzF) : nullptr, *dzT = gw ? h(w.dzT) : nullptr;
     if (!w.raw && w.pieces > 1) pack_piece<T>(w, r, n0, N, gh != nullptr, work, st);
     logits<T>(w, w.z, r, n0, N, rows, have_planes, work, [&](auto RAW) {
-      return EpiDz<decltype(RAW)::value, TERMS>{tg, lse, f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, r.ld_head, rows, 0.f};
+      return EpiDz<decltype(RAW)::value, TERMS>{tg, lse, f(w.ref), f(w.dz_coef), f(w.dz_max), n_max, dzF, dzT, w.Tp, N, w.V, n0, r.ld_head, rows, 0.f};
     }, st);
     const EpiHead head{w.head.slices, w.head_planes ? f(w.head_planes) : nullptr, w.Vp, w.dP, (T*)gw + (size_t)n0 * w.d, f32, w.d, rows,
                        f(w.dz_max), n_max, 0.f};
