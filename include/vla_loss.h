@@ -37,7 +37,7 @@ extern "C" {
 #endif
 
 /* Rows and head of a call.  Rows may be further apart than d_model (ld_*, in elements); both start on 16 bytes and ld is a
- * multiple of 16 bytes, at most 2^22 elements.  1 <= n_rows, vocab <= 2^20; d_model <= 2^15, a multiple of 8 (VLA_BF16) or 4 (VLA_F32). */
+ * multiple of 16 bytes, at most 2^22 elements.  1 <= n_rows <= 2^18, 1 <= vocab <= 2^20; d_model <= 2^15, a multiple of 8 (VLA_BF16) or 4 (VLA_F32). */
 typedef struct {
   const void* hidden;        /* device, [n_rows, d_model] */
   const void* head;          /* device, [vocab, d_model] */

@@ -153,8 +153,10 @@ struct RowsOut {
 };
 
 // Eight rows a workgroup, a wave each: the row's target and scale, then its h as operands; of few rows `splits` workgroups, which
-// take the chunks of columns in turn (each finds the scale for itself).  The workgroups behind those of the
-// rows pack the head (two tiles each), where a call packs it in one piece: a launch less.
+// take the chunks of columns in turn (each finds the scale for itself: 448 rows of 4096 11.4 -> 8.8 us).  The workgroups behind
+// those of the rows pack the head (two tiles each), where a call packs it in one piece: a launch less.  Bound by its chain of
+// latencies (5 to 9 us), and of thousands of rows by what it moves (8192 x 4096 36 us, 3.7 TB/s); a head of 32000 x 4096 packed both
+// ways 136 us with 2048 rows, 5.8 TB/s.
 constexpr int kRowsChunk = 1024;               // columns at a time
 constexpr int kRowsHeld = 4096;
 template <class T, int TERMS>
@@ -1101,7 +1103,7 @@ int check_rows(const vla_head_rows* r, bool pointers) {
   if (!r) return VLA_E_NULL;
   if (r->dtype != VLA_F32 && r->dtype != VLA_BF16) return VLA_E_CONFIG;
   const int unit = r->dtype == VLA_F32 ? 4 : 8;
-  if (r->n_rows < 1 || r->n_rows > 1 << 20 || r->vocab < 1 || r->vocab > 1 << 20) return VLA_E_SHAPE;
+  if (r->n_rows < 1 || r->n_rows > 1 << 18 || r->vocab < 1 || r->vocab > 1 << 20) return VLA_E_SHAPE;
   if (r->d_model < unit || r->d_model > 1 << 15 || r->d_model % unit) return VLA_E_SHAPE;
   if (!(r->temperature >= 0.f) || r->temperature > 3e38f) return VLA_E_SHAPE;
   if (!pointers) return VLA_OK;

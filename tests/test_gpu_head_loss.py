@@ -120,7 +120,14 @@ def test_lists_of_the_largest_length_in_one_corner_of_the_vocabulary():
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_pieces_of_the_vocabulary(dtype):
     """Sizes whose gradient takes several pieces, the last one not full."""
-    T, d, V = (1500, 64, 20001) if dtype == "f32" else (4100, 64, 20001)
+    T, d, V = (4500, 64, 20001) if dtype == "f32" else (8200, 64, 20001)
+    h, W, y, coef, _ = inputs(T, d, V, dtype)
+    check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
+
+
+@pytest.mark.parametrize("dtype,T,d,V", [("bf16", 20001, 64, 65), ("bf16", 40000, 64, 14000), ("f32", 17000, 72, 10001)])
+def test_many_rows(dtype, T, d, V):
+    """Rows whose coefficients are reduced by a launch of their own, and more pieces than sets of planes."""
     h, W, y, coef, _ = inputs(T, d, V, dtype)
     check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
 
