@@ -674,8 +674,8 @@ __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restric
   store_result(out, (size_t)m * d + c, out_f32, v * scale);
 }
 
-// Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in an order of their number and
-// hands to the epilogue, a workgroup 32 rows of 64 columns.
+// Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in their order and hands to the
+// epilogue, a workgroup 32 rows of 64 columns.
 template <int RAW>
 struct EpiPlanes {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -700,46 +700,36 @@ struct EpiPlanes {
 template <class Epi>
 __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restrict__ planes, int slices, int Tp, int N, int M, Epi epi_in) {
   constexpr int PITCH = 68;
-  __shared__ __attribute__((aligned(16))) float tiles[4][32 * PITCH];
+  __shared__ __attribute__((aligned(16))) float tile[32 * PITCH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int across = N / 64, m0 = blockIdx.x / across * 32, n0 = blockIdx.x % across * 64;
   Epi epi = epi_in;
-  const size_t plane = (size_t)Tp * N;
-  const float* p = planes + (size_t)(m0 + (lane >> 4)) * N + n0 + (lane & 15) * 4;
-  f32x4 v[8] = {};
-  for (int s = wave; s < slices; s += 16) {                          // every fourth slice a wave, four at a time
-    f32x4 u[4][8];
+  const size_t plane = (size_t)Tp * N, row4 = (size_t)4 * N;
+  const int r = wave * 8 + (lane >> 4), c4 = (lane & 15) * 4;        // eight rows a wave, in two halves
+  const float* p = planes + (size_t)(m0 + r) * N + n0 + c4;
+  f32x4 v[2] = {};
+  for (int s = 0; s < slices; s += 8) {                              // eight slices at a time
+    f32x4 u[8][2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 8; ++j)
+      if (s + j < slices) {
+        u[j][0] = *(const f32x4*)(p + (s + j) * plane);
+        u[j][1] = *(const f32x4*)(p + (s + j) * plane + row4);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (s + 4 * j < slices) u[j][i] = *(const f32x4*)(p + (s + 4 * j) * plane + (size_t)(4 * i) * N);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (s + 4 * j < slices) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += u[j][i];
+    for (int j = 0; j < 8; ++j)
+      if (s + j < slices) {
+        v[0] += u[j][0];
+        v[1] += u[j][1];
       }
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) *(f32x4*)(tiles[wave] + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4) = v[i];
+  *(f32x4*)(tile + r * PITCH + c4) = v[0];
+  *(f32x4*)(tile + (r + 4) * PITCH + c4) = v[1];
   if (wave < 2) {
     if constexpr (requires { epi.begin(lane); }) epi.begin(lane);
   }
   __syncthreads();
-  if (wave >= 2) return;
-  float* tile = tiles[0] + wave * 16 * PITCH;                        // 16 rows each of two waves
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float* x = tile + (4 * i + (lane >> 4)) * PITCH + (lane & 15) * 4;
-    f32x4 y = *(const f32x4*)x;
-#pragma unroll
-    for (int w = 1; w < 4; ++w) y += *(const f32x4*)(x + w * 32 * PITCH);
-    *(f32x4*)x = y;
-  }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-  __builtin_amdgcn_wave_barrier();
-  epi.template consume<64, PITCH, 16>(tile, m0 + wave * 16, n0, lane, M);
+  if (wave < 2) epi.template consume<64, PITCH, 16>(tile + wave * 16 * PITCH, m0 + wave * 16, n0, lane, M);
 }
 
 // grad_head: rows of a piece of the vocabulary.
@@ -871,7 +861,11 @@ struct EpiGradients {
 };
 
 static int round_up(int x, int n) { return (x + n - 1) / n * n; }
-static int tile_up(int x) { return x <= 128 ? 128 : round_up(x, 256); }        // columns of a product
+// Columns of a product: whole tiles of 256, or of 128 where that leaves more than an eighth less.
+static int tile_up(int x) {
+  const int a = round_up(x, 128), b = round_up(x, 256);
+  return 8 * (b - a) > b ? a : b;
+}
 
 // ---- tiles and slices -----------------------------------------------------------------------------------------------
 // Which tiles a product [M, N] over K takes, and into how many slices its contraction is split, goes by a model of its time: a
@@ -904,10 +898,11 @@ static float launch_us(int t, LossWork work, int M, int N, int K, int slices, bo
   return 2.0f + rounds * (c.fixed[work] + full * k) + (rest > 0.f ? c.fixed[work] + (few + (full - few) * rest) * k : 0.f);
 }
 // most: slices at most (1: not sliced).  Slices cost a launch that joins them and their planes, written and read at 4 TB/s.
+constexpr float kJoinUs[3] = {5.0f, 6.5f, 4.0f};
 static LossPick pick_tiles(LossWork work, int M, int N, int K, int most, bool raw) {
   LossPick best{L_64x128, 1, 1e30f};
   for (int s = 1; s <= most; s += s < 8 ? 1 : s < 16 ? 2 : 4) {
-    const float join = s > 1 ? 5.0f + kLossTiles[0].fixed[work] + (float)s * (float)M * (float)N * 2e-6f : 0.f;
+    const float join = s > 1 ? kJoinUs[work] + (float)s * (float)M * (float)N * 2e-6f : 0.f;
     if (join > best.us) break;
     for (int t = 0; t < (raw ? L_256x256 : L_COUNT); ++t) {
       if (N % kLossTiles[t].bn) continue;
@@ -1016,6 +1011,7 @@ struct Plan {
   bool raw;                    // the head is read as it is
   int piece, pieces;           // columns of the vocabulary at a time (gradient)
   LossPick z, stats;           // the logits' products (stats: of float32 with a gradient, which has both)
+  bool z_planes;               // they leave planes, for loss_slices_kernel
   LossPick hidden, head;
   int sets;                    // planes of grad_hidden: of each slice, of up to four pieces (later ones add to them)
   size_t z_scale, coef, dz_coef, dz_max, label, ids, p, ent, mass, first;
@@ -1034,8 +1030,11 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
     const size_t cols = (((size_t)512 << 20) / (2 * half * w.Tp)) & ~(size_t)255;
     const int most = cols < 256 ? 256 : cols > (size_t)w.Vp ? w.Vp : (int)cols;
     w.pieces = (w.Vp + most - 1) / most;
-    w.piece = w.pieces == 1 ? w.Vp : round_up((w.Vp + w.pieces - 1) / w.pieces, 256);
-    w.pieces = (w.Vp + w.piece - 1) / w.piece;
+    if (w.pieces > 1) {                                             // (every piece whole tiles of any kind)
+      w.Vp = round_up(w.V, 256);
+      w.piece = round_up((w.Vp + w.pieces - 1) / w.pieces, 256);
+      w.pieces = (w.Vp + w.piece - 1) / w.piece;
+    }
   }
   // Slices: a slab at least in each (of four, but for the last piece's).
   const int Kz = w.terms * w.dP, Kh = w.terms * w.piece, Kw = w.terms * w.Tp;
@@ -1043,8 +1042,21 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   auto most = [](int K) { return max(1, min(64, K / PK / 4)); };
   auto picks = [&](bool raw) {
     const int z_most = w.pieces > 1 ? 1 : raw ? most(w.d) : most(Kz);
-    w.z = pick_tiles(grad ? L_DZ : L_STATS, w.T, w.piece, raw ? w.d : Kz, z_most, raw);
-    w.stats = w.terms == 3 && grad ? w.z.slices > 1 ? w.z : pick_tiles(L_STATS, w.T, w.piece, Kz, 1, false) : w.z;
+    w.z = w.stats = pick_tiles(grad ? L_DZ : L_STATS, w.T, w.piece, raw ? w.d : Kz, z_most, raw);
+    w.z_planes = w.z.slices > 1;
+    if (w.terms == 3 && grad) {                  // two products, or one whose planes serve both (read twice)
+      w.z = pick_tiles(L_DZ, w.T, w.piece, Kz, 1, false), w.stats = pick_tiles(L_STATS, w.T, w.piece, Kz, 1, false);
+      float us = w.z.us + w.stats.us;
+      w.z_planes = false;
+      for (int s = 1; s <= z_most && w.pieces == 1; s += s < 8 ? 1 : s < 16 ? 2 : 4)
+        for (int t = 0; t < L_COUNT; ++t) {
+          if (w.piece % kLossTiles[t].bn) continue;
+          const float both = launch_us(t, L_STORE, w.T, w.piece, Kz, s, false) + kJoinUs[L_STATS] + kJoinUs[L_DZ] +
+                             (float)s * (float)w.T * (float)w.piece * 3e-6f;
+          if (both < us) us = both, w.z = w.stats = LossPick{t, s, both}, w.z_planes = true;
+        }
+      w.z.us = us;
+    }
     if (grad) w.hidden = pick_tiles(L_STORE, w.T, w.dP, Kh, min(most(Kh), last), raw);
     return (w.z.us + (grad ? w.hidden.us : 0.f)) * (float)w.pieces;
   };
@@ -1069,7 +1081,7 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   } else {
     w.label = take(4 * T);
   }
-  if (w.z.slices > 1) w.zp = take(4 * (size_t)w.z.slices * w.Tp * w.Vp);
+  if (w.z_planes) w.zp = take(4 * (size_t)w.z.slices * w.Tp * w.Vp);
   w.hF = take((size_t)w.Tp * w.dP * half);
   if (!w.raw) w.wF = take((size_t)w.piece * w.dP * half);
   if (!grad || w.terms == 3) w.pm = take(4 * T * w.groups), w.pl = take(4 * T * w.groups), w.pa = take(4 * T * (k ? k : 1));
@@ -1179,7 +1191,7 @@ void logits(const Plan& w, const LossPick& pick, const vla_head_rows& r, int n0,
   auto run = [&](auto RAW, int K) {
     constexpr int raw = decltype(RAW)::value;
     const auto epi = make(RAW);
-    if (pick.slices == 1) return product(pick.tile, hF, ld, W, w.T, N, K, epi, st);
+    if (!w.z_planes) return product(pick.tile, hF, ld, W, w.T, N, K, epi, st);
     if (!have_planes) product(pick.tile, hF, ld, W, w.T, N, K, EpiPlanes<raw>{pick.slices, zp, w.Tp, N, r.ld_head, rows}, st);
     hipLaunchKernelGGL((loss_slices_kernel<std::remove_const_t<decltype(epi)>>), dim3((w.Tp / 32) * (N / 64)), dim3(256), 0, st,
                        zp, pick.slices, w.Tp, N, w.T, epi);
@@ -1225,7 +1237,7 @@ int run_grad(const Plan& w, const vla_head_rows& r, const Targets& t, const floa
     statistics<T>(w, r, tg, nullptr, f(w.sum), f(w.ref), work, st);
     lse = f(w.sum);
   }
-  const bool have_planes = f32 && w.z.slices > 1;                    // (of the logits, from their statistics)
+  const bool have_planes = f32 && w.z_planes;                    // (of the logits, from their statistics)
   int n_max = w.Tp / 8;
   if (n_max > 2048) {
     hipLaunchKernelGGL(loss_max_kernel, dim3(1), dim3(256), 0, st, f(w.dz_max), n_max);
