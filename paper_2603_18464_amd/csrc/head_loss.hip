@@ -16,7 +16,11 @@
 // laid out as one contraction three times as long: [lo | hi | hi] against [hi | lo | hi], the small products first, so that their
 // sums are rounded at their own size.
 //
-// What bounds them: the large calls by the matrix cores (2 T V d operations forward, 6 backward).
+// What bounds them: the large calls by the matrix cores (2 T V d operations forward, 6 backward: 8192 rows of 32000 x 4096 1.36
+// PFLOP/s forward in all, 1.31 backward, where a library's plain product of 8192^3 reaches 1.23), few rows by reading the head (once
+// forward; twice and written once backward), the smallest by three to six launches of 4 to 10 us each.  The logits are never
+// written: a tile's statistics, or its dz, are formed from the accumulators.  Keeping dz rather than forming z a second time for each
+// product costs 2 T V bytes each way instead of 2 T V d operations.
 #include "gemm_tile.h"
 #include "../../include/vla_loss.h"
 
@@ -387,7 +391,10 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
 
 // ---- epilogues -----------------------------------------------------------------------------------------------
 // Partial statistics of the groups of 64 columns.  ROWS rows of a group by 64 / ROWS lanes each; a group's sums are formed in
-// the same order whatever the tile, so a row's loss does not depend on the rows beside it.
+// the same order whatever the tile.  What rows hold does not reach the rows beside them (their number picks the tile and the
+// slices, by which sums of products may be rounded otherwise).
+// Bound by the matrix cores: 8192 x 32000 x 4096 1.5 ms, 1.43 PFLOP/s (256x256 tiles); with d 768 by this epilogue too (2301 rows 114
+// us, 0.99); one row by reading the head as it is (40 us, 6.5 TB/s, a part of it from the last-level cache).
 // EXACT (float32): t in place of l, from differences to the largest that are exact where they are small.
 template <int RAW, bool EXACT>
 struct EpiStats {
@@ -472,6 +479,9 @@ __device__ __forceinline__ float from_largest(float x, float z_scale, float m) {
 }
 // dz as the operand of both gradient products: rows (F, times 2^15) and transposed (FT, times the rows' coefficients and what
 // brings them all to 2^15).  Rows T .. Tp and columns V .. are zeros.
+// Bound by the matrix cores and by itself, for all tiles of a round store at the same time: 8192 x 16128 x 4096 0.89 ms, 1.22
+// PFLOP/s; a round of 256x256 tiles ends with 16 us of this, 9 of statistics.  Four waves of 128x128 and
+// loads that are not spread gained nothing, waves of 128x64 lost.
 template <int RAW, int TERMS>
 struct EpiDz {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -619,6 +629,7 @@ __device__ __forceinline__ void store_result(void* out, size_t at, bool f32, con
 }
 
 // grad_hidden of one slice of the vocabulary: a plane of float32 sums, or, where there is only one, the result.
+// 8192 x 4096 x 16128 0.74 ms, 1.46 PFLOP/s; 56 x 4096 x 32000 44 us, 6.0 TB/s of the head as it is.
 template <int RAW>
 struct EpiHidden {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -651,7 +662,8 @@ struct EpiHidden {
     }
   }
 };
-// ... and the planes in their order, times the rows' coefficients or (nullptr) what grad_head takes.
+// ... and the planes in their order, times the rows' coefficients or (nullptr) what grad_head takes.  Bound by what it moves: two
+// planes of 8192 x 4096 53 us, 6.3 TB/s.
 __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restrict__ planes, int n, int plane_rows, int ld, int rows,
                                                           int d, const float* __restrict__ coef, const float* __restrict__ dz_max,
                                                           int n_max, void* __restrict__ out, int out_f32) {
@@ -675,7 +687,8 @@ __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restric
 }
 
 // Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in their order and hands to the
-// epilogue, a workgroup 32 rows of 64 columns.
+// epilogue, a workgroup 32 rows of 64 columns.  448 rows of 256 bins over
+// 4096: 28 tiles of 64x128 in four slices 6.0 us, this 5.8.
 template <int RAW>
 struct EpiPlanes {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -732,7 +745,7 @@ __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restric
   if (wave < 2) epi.template consume<64, PITCH, 16>(tile + wave * 16 * PITCH, m0 + wave * 16, n0, lane, M);
 }
 
-// grad_head: rows of a piece of the vocabulary.
+// grad_head: rows of a piece of the vocabulary.  16128 x 4096 x 8192 0.78 ms, 1.39 PFLOP/s; 32003 x 768 x 1021 51 us (49 MB written).
 struct EpiHead {
   static constexpr int kSpan = 64;
   static constexpr bool kSliced = true;                // (of the rows)
@@ -764,7 +777,8 @@ struct EpiHead {
 // grad_head of at most 128 rows (bfloat16), where it is bound by what it writes: 64 rows of the head by 64 columns at a time a
 // wave, whose dz stays in registers while it walks `walk` columns, straight from the accumulators.  The products are transposed (a row
 // of dz^T is a column here), and which columns of h a tile's rows are is chosen so that a lane holds eight in a row of each two
-// tiles, and the four groups of lanes 64 bytes.
+// tiles, and the four groups of lanes 64 bytes; lanes of rows 8 apart swap halves, so that a store covers 128.  32000 x 4096 of 56
+// rows: 262 MB in 50 to 54 us, 5 TB/s (a large copy 4.8); by the products' tiles 81.
 template <int KS>
 __global__ __launch_bounds__(256) void loss_head_rows_kernel(const f16* __restrict__ dzT, const f16* __restrict__ hT, int Tp,
                                                              const float* __restrict__ dz_max, int n_max, bf16* __restrict__ out,
@@ -940,7 +954,7 @@ static void gradients(const f16* A, int lda, const f16* W, int M, int N, int K, 
 }
 
 // ---- joining the groups -------------------------------------------------------------------------------------------
-// (EXACT as above.)  16 rows a workgroup, 64 threads a row, which take every 64th group; their sums are joined in a tree.
+// (EXACT as above.)  Bound by latency (3 to 5 us; 8192 rows of 500 groups 14).  16 rows a workgroup, 64 threads a row, which take every 64th group; their sums are joined in a tree.
 template <bool EXACT>
 __global__ __launch_bounds__(1024) void loss_join_kernel(const float* __restrict__ pm, const float* __restrict__ pl,
                                                          const float* __restrict__ pa, int T, int groups, RowTargets tg,
@@ -1062,9 +1076,10 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   };
   const float packed = picks(false);
   // A bfloat16 head is read as it is where packing it (5 TB/s of twice its bytes, three times with a gradient) costs more.  us, as
-  // it is / packed, loss and gradient: 32000 x 4096 56 rows 57 / 148, 238 / 365, 384 rows 112 / 185, 425 / 525, 768 rows 202 / 258,
-  // 653 / 728, 1536 rows 404 / 391, 1196 / 1148; 32000 x 768 56 rows 21 / 34, 54 / 73, 256 rows 31 / 39, 92 / 96, 512 rows 57 / 50,
-  // 160 / 133; 8000 x 2048 256 rows 30 / 31, 70 / 71, 384 rows 45 / 35, 101 / 84; 4000 x 1024 the same within 5 % up to 384 rows.
+  // it is / packed, loss and gradient (with one form of grad_head): 32000 x 4096 56 rows 57 / 148, 238 / 365, 384 rows 112 / 185,
+  // 425 / 525, 768 rows 202 / 258, 653 / 728, 1536 rows 404 / 391, 1196 / 1148; 32000 x 768 56 rows 21 / 34, 54 / 73, 256 rows 31 /
+  // 39, 92 / 96, 512 rows 57 / 50, 160 / 133; 8000 x 2048 256 rows 30 / 31, 70 / 71, 384 rows 45 / 35, 101 / 84; 4000 x 1024 the
+  // same within 5 % up to 384 rows.
   if (r.dtype == VLA_BF16 && w.d % PK == 0) {
     const float raw = picks(true);
     w.raw = raw < packed + (float)w.V * (float)w.d * (grad ? 6e-6f : 4e-6f) / 5.0f;
