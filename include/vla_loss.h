@@ -44,7 +44,7 @@ typedef struct {
   int64_t ld_hidden, ld_head;
   int32_t n_rows, d_model, vocab;
   int32_t dtype;             /* enum vla_dtype */
-  float temperature;         /* finite, >= 0 */
+  float temperature;         /* 0 (as 1), or between 2^-40 and 2^40 */
 } vla_head_rows;
 
 /* Teacher's entries of the distillation calls: n_top in [1, 1024], logits and ids [n_rows, n_top] without gaps. */

@@ -209,10 +209,10 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
     live = target >= 0 && target < V;
     if (lane == 0 && first) out.label[row] = live ? target : -1;
   } else if (!first) {
-    bool any = target >= 0 && target < V && first_logit * inv_tau != -INFINITY;
+    bool any = target >= 0 && target < V && first_logit != -INFINITY;
     for (int j = lane + 64; j < k; j += 64) {
       const int32_t id = top_ids[(size_t)row * k + j];
-      any = any || (id >= 0 && id < V && top_logits[(size_t)row * k + j] * inv_tau != -INFINITY);
+      any = any || (id >= 0 && id < V && top_logits[(size_t)row * k + j] != -INFINITY);
     }
     live = __any(any);
   } else {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
       float l = 0.f;
       if (j < k) {
         id = j < 64 ? target : top_ids[(size_t)row * k + j];
-        l = (j < 64 ? first_logit : top_logits[(size_t)row * k + j]) * inv_tau;
+        l = j < 64 ? first_logit : top_logits[(size_t)row * k + j];
         if (id < 0 || id >= V || l == -INFINITY) id = -1;
       }
       s_id[j] = id;
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(512) void loss_rows_kernel(const T* __restrict__ h,
     m = m == -INFINITY ? 0.f : m;                                    // (all NaN, or none)
     float sum = 0.f;
     for (int j = lane; j < kp; j += 64) {
-      const float e = s_id[j] >= 0 ? expf(s_p[j] - m) : 0.f;
+      const float e = s_id[j] >= 0 ? expf((s_p[j] - m) * inv_tau) : 0.f;   // (the difference first: no logit overflows)
       s_p[j] = e;
       sum += e;
     }
@@ -480,8 +480,8 @@ __device__ __forceinline__ float from_largest(float x, float z_scale, float m) {
 // dz as the operand of both gradient products: rows (F, times 2^15) and transposed (FT, times the rows' coefficients and what
 // brings them all to 2^15).  Rows T .. Tp and columns V .. are zeros.
 // Bound by the matrix cores and by itself, for all tiles of a round store at the same time: 8192 x 16128 x 4096 0.89 ms, 1.22
-// PFLOP/s; a round of 256x256 tiles ends with 16 us of this, 9 of statistics.  Four waves of 128x128 and
-// loads that are not spread gained nothing, waves of 128x64 lost.
+// PFLOP/s; a round of 256x256 tiles ends with 16 us of this, 9 of statistics.  Four waves of 128x128 and loads that are not spread
+// gained nothing, waves of 128x64 lost.
 template <int RAW, int TERMS>
 struct EpiDz {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -687,8 +687,7 @@ __global__ __launch_bounds__(256) void loss_planes_kernel(const float* __restric
 }
 
 // Products of few tiles and a long contraction are sliced: planes of float32 sums, which this adds in their order and hands to the
-// epilogue, a workgroup 32 rows of 64 columns.  448 rows of 256 bins over
-// 4096: 28 tiles of 64x128 in four slices 6.0 us, this 5.8.
+// epilogue, a workgroup 32 rows of 64 columns.  448 rows of 256 bins over 4096: 28 tiles of 64x128 in four slices 6.0 us, this 5.8.
 template <int RAW>
 struct EpiPlanes {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -1132,7 +1131,7 @@ int check_rows(const vla_head_rows* r, bool pointers) {
   const int unit = r->dtype == VLA_F32 ? 4 : 8;
   if (r->n_rows < 1 || r->n_rows > 1 << 18 || r->vocab < 1 || r->vocab > 1 << 20) return VLA_E_SHAPE;
   if (r->d_model < unit || r->d_model > 1 << 15 || r->d_model % unit) return VLA_E_SHAPE;
-  if (!(r->temperature >= 0.f) || r->temperature > 3e38f) return VLA_E_SHAPE;
+  if (r->temperature != 0.f && !(r->temperature >= 0x1p-40f && r->temperature <= 0x1p40f)) return VLA_E_SHAPE;
   if (!pointers) return VLA_OK;
   if (!r->hidden || !r->head) return VLA_E_NULL;
   if (r->ld_hidden < r->d_model || r->ld_head < r->d_model || r->ld_hidden > 1 << 22 || r->ld_head > 1 << 22 || r->ld_hidden % unit || r->ld_head % unit) return VLA_E_SHAPE;

@@ -104,8 +104,8 @@ def _grad(name, hidden, head, targets, n_top, lse, grad_loss, temperature, want_
 
 
 def token_loss(hidden, head, labels, temperature: float = 0.0, work: Optional[torch.Tensor] = None):
-    """(loss, lse) [rows] float32 of labels [rows] int32: lse - z[label], z = hidden head^T / temperature (0 means 1).
-    A label outside [0, vocab): no target, 0."""
+    """(loss, lse) [rows] float32 of labels [rows] int32: lse - z[label], z = hidden head^T / temperature (0 means 1, others lie
+    between 2^-40 and 2^40).  A label outside [0, vocab): no target, 0."""
     return _loss("vla_token_loss", hidden, head, *_labels(hidden, labels), temperature, work)
 
 

@@ -172,6 +172,18 @@ def test_scales(dtype):
     check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
 
 
+@pytest.mark.parametrize("tau", [0.5, 2.0 ** -40, 2.0 ** 40])
+def test_teacher_logits_at_the_ends_of_their_type(tau):
+    """The lowest and highest finite logits are entries like any other, whatever the temperature makes of them."""
+    h, W, _, coef, _ = inputs(5, 64, 70, "bf16")
+    h *= min(tau, 1.0)
+    low, high = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    logits = torch.tensor([[low, low], [low, 0.0], [high, high], [high, low], [low, -math.inf]], device=DEV)
+    ids = torch.tensor([[3, 69], [0, 64], [1, 1], [8, 7], [65, 2]], dtype=torch.int32, device=DEV)
+    got = call("distill", h, W, (logits, ids), tau, coef)
+    check("distill", h, W, (logits, ids), tau, coef, got)
+
+
 def test_no_row_has_a_target():
     h, W, y, coef, _ = inputs(40, 128, 300, "bf16")
     h[:] = math.nan

@@ -81,7 +81,8 @@ def calls(r, work=4096, size=1 << 40, top=4, **null):
     (dict(n_rows=0), -3), (dict(n_rows=-1), -3), (dict(n_rows=(1 << 18) + 1), -3), (dict(vocab=0), -3), (dict(vocab=(1 << 20) + 1), -3),
     (dict(d_model=0), -3), (dict(d_model=60), -3), (dict(d_model=(1 << 15) + 8, ld_hidden=1 << 16, ld_head=1 << 16), -3),
     (dict(dtype=2), -2), (dict(dtype=-1), -2), (dict(temperature=-1.0), -3), (dict(temperature=math.nan), -3),
-    (dict(temperature=math.inf), -3), (dict(hidden=None), -1), (dict(head=None), -1), (dict(ld_hidden=56), -3), (dict(ld_head=0), -3),
+    (dict(temperature=math.inf), -3), (dict(temperature=1e-39), -3), (dict(temperature=2.0 ** -41), -3), (dict(temperature=2.0 ** 41), -3),
+    (dict(hidden=None), -1), (dict(head=None), -1), (dict(ld_hidden=56), -3), (dict(ld_head=0), -3),
     (dict(ld_head=65), -3), (dict(ld_hidden=68), -3), (dict(hidden=258), -3), (dict(head=520), -3),
     (dict(dtype=B.VLA_F32, d_model=62), -3), (dict(dtype=B.VLA_F32, ld_head=66), -3),
 ])
