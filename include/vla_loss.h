@@ -22,7 +22,8 @@
  * the size vla_loss_workspace names; nothing in it has to survive between calls, and calls that may overlap in time (other
  * streams, captured graphs that are replayed side by side) need one each.  Outputs must not overlap inputs.  Results do not depend
  * on timing: no sum's order is left to chance.
- *   VLA_F32   float32 in and out; products of about 22 significant bits, accumulated in float32.
+ *   VLA_F32   float32 in and out; products of about 22 significant bits, accumulated in float32.  A row's share of grad_head is
+ *             carried in steps of 2^-37 of the largest |grad_loss h| of all rows where that is more (VLA_BF16 too).
  *   VLA_BF16  h, W and the gradients bfloat16; inside, half precision with power-of-two scales (exact for h, per row, and for
  *             2^-25 <= |W| <= 255 as in vla_load_weights; a larger |W| or one that is not finite makes the losses NaN), dz
  *             rounded to half precision, everything accumulated in float32.

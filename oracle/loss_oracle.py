@@ -85,5 +85,11 @@ class Loss:
         hc = self.h * c[:, None]
         gw, ahc = dz.T @ hc, hc.abs()                                  # h g: its own rounding, in steps of 2^-38 of its maximum
         bw = (e + adz * (more + step + (T / 4 + 16) * F32)).T @ ahc + (adz + e).sum(0)[:, None] * 2.0 ** -37 * ahc.max()
+        # dz g as the first factor of grad_head has one scale for all rows, that of the largest c |h|: row t carries
+        # x = dz 2^15 c_t 2^-e_t f, f a power of two that brings the largest c 2^-e into [1/2, 1), against h_t 2^e_t, at most 2^14,
+        # whose largest in the row is at least 2^13.  Below half precision's normal numbers x is off by up to half a step of
+        # 2^-24 (two terms: the low one by that), so that row t is off by 2^-25 2^14 / (2^15 f), and 1 / f is at most
+        # 2 max |c| 2^-e <= 2 max |c h| 2^-13: 2^-38 max |c h| a row, however small its own c and dz are.
+        bw = bw + float(self.live.sum()) * 2.0 ** -38 * ahc.max()
         out = OUT[self.dtype] * 1.01 + 6 * F32                         # (and of g / tau and the products with it)
         return (gh, bh + gh.abs() * out + 1e-40), (gw, bw + gw.abs() * out + 1e-40)

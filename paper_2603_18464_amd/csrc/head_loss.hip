@@ -11,7 +11,8 @@
 // All products run on the half-precision kernel of gemm_tile.h.  Powers of two keep operands in the range of half precision: a
 // row of h is scaled to a maximum in [2^13, 2^14) (exact for bfloat16), W by 2^8 (exact, as in the arena), dz, which lies in
 // [-1, 1], by 2^15 for grad_hidden, whose rows take their g / tau at the end, and times g / tau over the row's scale as one tensor
-// to a maximum of 2^15 for grad_head.  dz is rounded to half precision (2^-11 of its value at most); everything else is float32.
+// to a maximum of 2^15 for grad_head.  dz is rounded to half precision (2^-11 of its value at most, or 2^-40, for
+// grad_head 2^-38 of the largest row's g h, where that is more: below the normal numbers); everything else is float32.
 // float32 operands are carried as two terms hi + lo (22 bits); a product of two of them is three, hi hi + lo hi + hi lo,
 // laid out as one contraction three times as long: [lo | hi | hi] against [hi | lo | hi], the small products first, so that their
 // sums are rounded at their own size.

@@ -172,6 +172,16 @@ def test_scales(dtype):
     check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind,T,d,V", [("token", 3, 920, 3674), ("distill", 2, 64, 12637), ("token", 40, 128, 300)])
+def test_very_sharp_rows(kind, T, d, V, dtype):
+    """Rows whose logits span hundreds of nats, coefficients that span six orders."""
+    h, W, y, coef, g = inputs(T, d, V, dtype, scale=30.0)
+    coef = coef * 10.0 ** (-6 * torch.rand(T, generator=g)).to(DEV)
+    tgt = (y,) if kind == "token" else teacher(T, V, 20, g)
+    check(kind, h, W, tgt, 0.7, coef, call(kind, h, W, tgt, 0.7, coef))
+
+
 @pytest.mark.parametrize("tau", [0.5, 2.0 ** -40, 2.0 ** 40])
 def test_teacher_logits_at_the_ends_of_their_type(tau):
     """The lowest and highest finite logits are entries like any other, whatever the temperature makes of them."""
