@@ -1040,8 +1040,14 @@ Plan make_plan(const vla_head_rows& r, int k, bool grad) {
   w.groups = (w.V + kGroup - 1) / kGroup;
   const size_t half = 2 * (size_t)w.terms;
   w.piece = w.Vp, w.pieces = 1;
-  if (grad) {                                                       // dz, both ways, within 512 MB
-    const size_t cols = (((size_t)512 << 20) / (2 * half * w.Tp)) & ~(size_t)255;
+  if (grad) {
+    // dz, both ways, is whole within 2 GB.  Otherwise it is formed in pieces: each reads and writes the planes of grad_hidden (8 d
+    // bytes a row, against 8 a column of dz), so that a piece has 16 d columns, within 512 MB and 2 GB.  us, pieces within 512 MB,
+    // 1 GB, 2 GB, and 4 GB of dz: 6171 x 28990 x 512 877, 673 (whole); 8192 x 32000 x 4096 4957, 4847 (whole); 32768 x 32000 x 768
+    // 8020, 5697, 4794, 4684; 65536 x 32000 x 1024 30558, 18558, 13046, 11078; 20000 x 32000 x 4096 12782, 12171, 11882, 11770.
+    // (Less than 512 MB is slower as well, although it would stay in the last-level cache.)
+    const size_t column = 2 * half * w.Tp, low = (size_t)512 << 20, high = (size_t)2 << 30, by_d = 16 * column * w.dP;
+    const size_t cols = ((column * w.Vp <= high || by_d > high ? high : by_d < low ? low : by_d) / column) & ~(size_t)255;
     const int most = cols < 256 ? 256 : cols > (size_t)w.Vp ? w.Vp : (int)cols;
     w.pieces = (w.Vp + most - 1) / most;
     if (w.pieces > 1) {                                             // (every piece whole tiles of any kind)

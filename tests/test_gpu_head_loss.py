@@ -125,6 +125,14 @@ def test_pieces_of_the_vocabulary(dtype):
     check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
 
 
+@pytest.mark.parametrize("dtype,T,d,V", [("bf16", 27000, 64, 20001), ("f32", 21000, 72, 9001), ("bf16", 9000, 384, 61000)])
+def test_pieces_of_large_calls(dtype, T, d, V):
+    """Calls whose dz is more than two gigabytes: pieces by the smallest limit, more than sets of planes, and by d."""
+    h, W, y, coef, _ = inputs(T, d, V, dtype)
+    y[::5] = V
+    check("token", h, W, (y,), 0.0, coef, call("token", h, W, (y,), 0.0, coef))
+
+
 @pytest.mark.parametrize("dtype,T,d,V", [("bf16", 20001, 64, 65), ("bf16", 40000, 64, 14000), ("f32", 17000, 72, 10001)])
 def test_many_rows(dtype, T, d, V):
     """Rows whose coefficients are reduced by a launch of their own, and more pieces than sets of planes."""
