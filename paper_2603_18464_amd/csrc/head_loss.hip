@@ -47,6 +47,24 @@ struct RowTargets {
 #pragma unroll
     for (int i = 0; i < N; ++i) at[i] = first[(size_t)m * (groups + 1) + min(g + i, groups)];
   }
+  // use(e, id, probability) of entries from .. to - 1 of row m, four requested at a time (one after the other each would wait for
+  // its own loads, which use()'s stores keep behind them).
+  template <class Use>
+  __device__ __forceinline__ void each(int m, int from, int to, Use&& use) const {
+    for (int e = from; e < to; e += 4) {
+      int id[4];
+      float pr[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const size_t at = (size_t)m * k + min(e + j, to - 1);
+        id[j] = ids[at];
+        pr[j] = p[at];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (e + j < to) use(e + j, id[j], pr[j]);
+    }
+  }
 };
 
 template <class T> struct Vec;
@@ -459,10 +477,9 @@ struct EpiStats {
           const int c = label - n0;
           if (c >= 0 && c < kGroup) pa[m] = tile[r * PITCH + gg * kGroup + c] * zs;
         } else {
-          for (int e = entry[gg]; e < entry[gg + 1]; ++e) {
-            const size_t at = (size_t)m * tg.k + e;
-            pa[at] = tg.p[at] * (tile[r * PITCH + gg * kGroup + tg.ids[at] - n0] * zs);
-          }
+          tg.each(m, entry[gg], entry[gg + 1], [&](int e, int id, float p) __attribute__((always_inline)) {
+            pa[(size_t)m * tg.k + e] = p * (tile[r * PITCH + gg * kGroup + id - n0] * zs);
+          });
         }
         const size_t at = (size_t)(n0 / kGroup) * T + m;
         pm[at] = mx == -INFINITY ? mx : mx * zs;
@@ -575,12 +592,11 @@ struct EpiDz {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
       __builtin_amdgcn_wave_barrier();
       if (part == 0 && live)
-        for (int e = entry[0]; e < entry[COLS / kGroup]; ++e) {
-          const size_t at = (size_t)m * tg.k + e;
-          float* x = &tile[r * PITCH + tg.ids[at] - n_base - nb];
-          if constexpr (own) *x = *x == scale ? fmaf(1.0f - tg.p[at], kDzScale, top) : fmaf(tg.p[at], -kDzScale, *x);
-          else *x = fmaf(tg.p[at], -kDzScale, *x);
-        }
+        tg.each(m, entry[0], entry[COLS / kGroup], [&](int, int id, float p) __attribute__((always_inline)) {
+          float* x = &tile[r * PITCH + id - n_base - nb];
+          if constexpr (own) *x = *x == scale ? fmaf(1.0f - p, kDzScale, top) : fmaf(p, -kDzScale, *x);
+          else *x = fmaf(p, -kDzScale, *x);
+        });
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
