@@ -497,7 +497,7 @@ __device__ __forceinline__ float from_largest(float x, float z_scale, float m) {
 }
 // dz as the operand of both gradient products: rows (F, times 2^15) and transposed (FT, times the rows' coefficients and what
 // brings them all to 2^15).  Rows T .. Tp and columns V .. are zeros.
-// Bound by the matrix cores and by itself, for all tiles of a round store at the same time: 8192 x 16128 x 4096 0.89 ms, 1.22
+// Bound by the matrix cores and by itself, for all tiles of a round store at the same time: 8192 x 32000 x 4096 1.78 ms, 1.21
 // PFLOP/s; a round of 256x256 tiles ends with 16 us of this, 9 of statistics.  Four waves of 128x128 and loads that are not spread
 // gained nothing, waves of 128x64 lost.
 template <int RAW, int TERMS>
@@ -646,7 +646,7 @@ __device__ __forceinline__ void store_result(void* out, size_t at, bool f32, con
 }
 
 // grad_hidden of one slice of the vocabulary: a plane of float32 sums, or, where there is only one, the result.
-// 8192 x 4096 x 16128 0.74 ms, 1.46 PFLOP/s; 56 x 4096 x 32000 44 us, 6.0 TB/s of the head as it is.
+// 8192 x 4096 x 32000 1.45 ms, 1.48 PFLOP/s; 56 x 4096 x 32000 44 us, 6.0 TB/s of the head as it is.
 template <int RAW>
 struct EpiHidden {
   static constexpr int kSpan = 64, kRaw = RAW;
@@ -761,7 +761,7 @@ __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restric
   if (wave < 2) epi.template consume<64, PITCH, 16>(tile + wave * 16 * PITCH, m0 + wave * 16, n0, lane, M);
 }
 
-// grad_head: rows of a piece of the vocabulary.  16128 x 4096 x 8192 0.78 ms, 1.39 PFLOP/s; 32003 x 768 x 1021 51 us (49 MB written).
+// grad_head: rows of a piece of the vocabulary.  32000 x 4096 x 8192 1.65 ms, 1.30 PFLOP/s; 32003 x 768 x 1021 51 us (49 MB written).
 struct EpiHead {
   static constexpr int kSpan = 64;
   static constexpr bool kSliced = true;                // (of the rows)
